@@ -35,6 +35,11 @@ DEBUG_EXPORTS = ("moe_debug_gemm_units", "moe_debug_ffn_plan", "moe_debug_down_s
                  "moe_debug_tile_rows", "moe_debug_even_units", "moe_debug_tall", "moe_debug_tall_units",
                  "moe_debug_flow", "moe_debug_flow_place", "moe_debug_flow_tiles", "moe_debug_walk_split")
 INT4_EXPORTS = ("moe_int4_dequantize", "moe_int4_quantize")
+LORA_EXPORTS = ("moe_lora_forward", "moe_lora_backward", "moe_lora_workspace_bytes")
+ROUTER_GRAD_EXPORTS = ("moe_balance_loss", "moe_balance_workspace_bytes", "moe_route_backward", "moe_router_backward",
+                       "moe_router_backward_workspace_bytes", "moe_combine_backward")
+MOE_LORA_MAX_ADAPTERS = 256
+MOE_LORA_MAX_RANK = 128
 INT4_GROUP = 64
 DEBUG_UNIT_INTS = 5
 DEBUG_SLICE_INTS = 8
@@ -99,6 +104,25 @@ def lib() -> ctypes.CDLL:
         L.moe_int4_dequantize.restype = ctypes.c_int
         L.moe_int4_quantize.argtypes = [vp, ctypes.c_int64, vp, vp, vp]
         L.moe_int4_quantize.restype = ctypes.c_int
+        f32 = ctypes.c_float
+        L.moe_lora_forward.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, u32, vp]
+        L.moe_lora_forward.restype = ctypes.c_int
+        L.moe_lora_backward.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.moe_lora_backward.restype = ctypes.c_int
+        L.moe_lora_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+        L.moe_lora_workspace_bytes.restype = sz
+        L.moe_balance_loss.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.moe_balance_loss.restype = ctypes.c_int
+        L.moe_balance_workspace_bytes.argtypes = [i32, i32]
+        L.moe_balance_workspace_bytes.restype = sz
+        L.moe_route_backward.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, f32, f32, u32, vp, vp]
+        L.moe_route_backward.restype = ctypes.c_int
+        L.moe_router_backward.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.moe_router_backward.restype = ctypes.c_int
+        L.moe_router_backward_workspace_bytes.argtypes = [i32, i32, i32]
+        L.moe_router_backward_workspace_bytes.restype = sz
+        L.moe_combine_backward.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, u32, vp]
+        L.moe_combine_backward.restype = ctypes.c_int
         L.moe_debug_ffn_plan.argtypes = [i32, shp, vp]
         L.moe_debug_ffn_plan.restype = i32
         L.moe_debug_walk_split.argtypes = [i32, i32, i32, vp]
@@ -224,6 +248,64 @@ def moe_int4_dequantize(codes, qparams, n_elems, w_bf16, stream=None):
 def moe_int4_quantize(w_bf16, n_elems, codes, qparams, stream=None):
     _check("moe_int4_quantize", lib().moe_int4_quantize(_ptr(w_bf16), n_elems, _ptr(codes), _ptr(qparams),
                                                         _stream(stream)))
+
+
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def moe_lora_workspace_bytes(T, K, N, rank, n_adapters, backward=False) -> int:
+    return int(lib().moe_lora_workspace_bytes(T, K, N, rank, n_adapters, int(backward)))
+
+
+def moe_lora_forward(x, adapter_idx, T, K, N, rank, n_adapters, lora_a, lora_b, scale, y_in, y_out, v=None, workspace=None,
+                     flags=0, stream=None):
+    _check("moe_lora_forward",
+           lib().moe_lora_forward(_ptr(x), _ptr(adapter_idx), T, K, N, rank, n_adapters, _ptr(lora_a), _ptr(lora_b),
+                                  _ptr(scale), _ptr(y_in), _ptr(y_out), _ptr(v), _ptr(workspace), _bytes(workspace), flags,
+                                  _stream(stream)))
+
+
+def moe_lora_backward(x, dy, adapter_idx, T, K, N, rank, n_adapters, lora_a, lora_b, scale, v, dx_in, dx, grad_a, grad_b,
+                      workspace=None, stream=None):
+    _check("moe_lora_backward",
+           lib().moe_lora_backward(_ptr(x), _ptr(dy), _ptr(adapter_idx), T, K, N, rank, n_adapters, _ptr(lora_a),
+                                   _ptr(lora_b), _ptr(scale), _ptr(v), _ptr(dx_in), _ptr(dx), _ptr(grad_a), _ptr(grad_b),
+                                   _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def moe_balance_workspace_bytes(T, E) -> int:
+    return int(lib().moe_balance_workspace_bytes(T, E))
+
+
+def moe_balance_loss(logits, topk_idx, token_mask, T, E, k, counts, mean_prob, losses, workspace=None, stream=None):
+    _check("moe_balance_loss",
+           lib().moe_balance_loss(_ptr(logits), _ptr(topk_idx), _ptr(token_mask), T, E, k, _ptr(counts), _ptr(mean_prob),
+                                  _ptr(losses), _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def moe_route_backward(logits, topk_idx, d_topk_w, token_mask, counts, T, E, k, coef_balance, coef_z, flags, d_logits,
+                       stream=None):
+    _check("moe_route_backward",
+           lib().moe_route_backward(_ptr(logits), _ptr(topk_idx), _ptr(d_topk_w), _ptr(token_mask), _ptr(counts), T, E, k,
+                                    coef_balance, coef_z, flags, _ptr(d_logits), _stream(stream)))
+
+
+def moe_router_backward_workspace_bytes(T, H, E) -> int:
+    return int(lib().moe_router_backward_workspace_bytes(T, H, E))
+
+
+def moe_router_backward(x, w_router, d_logits, T, H, E, dx_in, dx, d_w_router, workspace=None, stream=None):
+    _check("moe_router_backward",
+           lib().moe_router_backward(_ptr(x), _ptr(w_router), _ptr(d_logits), T, H, E, _ptr(dx_in), _ptr(dx),
+                                     _ptr(d_w_router), _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def moe_combine_backward(dy, y_perm, slot_row, T, k, H, y_shared, x, w_shared_gate, d_topk_w, d_shared_gate=None, flags=0,
+                         stream=None):
+    _check("moe_combine_backward",
+           lib().moe_combine_backward(_ptr(dy), _ptr(y_perm), _ptr(slot_row), T, k, H, _ptr(y_shared), _ptr(x),
+                                      _ptr(w_shared_gate), _ptr(d_topk_w), _ptr(d_shared_gate), flags, _stream(stream)))
 
 
 def moe_debug_gemm_units(expert_offsets, cap_rows, n_col_blocks):
