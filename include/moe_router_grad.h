@@ -10,7 +10,7 @@
  *
  * Conventions as in moe_shard.h: status codes (MOE_OK / MOE_ERR_*), validation on the host before any HIP call, no allocation, no
  * synchronisation, work enqueued on `stream`; all pointers are DEVICE pointers owned by the caller.  With T == 0 the buffers of T rows may be NULL.  bf16 tensors, y_perm,
- * y_shared, w_shared_gate and workspaces are 16-byte aligned.  A call writes all of its workspace that it reads, so nothing
+ * y_shared, w_shared_gate, d_w_router and workspaces are 16-byte aligned.  A call writes all of its workspace that it reads, so nothing
  * has to start at zero; calls that overlap on one GPU each bring their own.  Sums are taken in a fixed order: the same call gives the
  * same bits.
  */

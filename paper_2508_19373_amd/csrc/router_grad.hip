@@ -2,190 +2,389 @@
 // router's weights.
 #include <cmath>
 
-#include "moe_internal.hpp"
 #include "moe_router_grad.h"
+#include "skinny.hpp"
 
 namespace moe {
 namespace {
 
+using namespace skinny;
+
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kSlots = MOE_MAX_EXPERTS / kWave;
 
-// softmax of one token's row: expert lane + 64 s in slot s; returns log sum exp
-__device__ __forceinline__ float row_softmax(const float* __restrict__ row, int lane, int E, float (&p)[kSlots]) {
-  float top = -INFINITY;
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// ---- softmax rows ----------------------------------------------------------------------------------------------------------
+// G lanes (8 to 64) share a token and its E experts, expert l + G s in slot s of the group's lane l: with 8 experts a wavefront holds
+// eight tokens, with 60 one, and every load is of neighbouring words.
+template <int G, typename Op>
+__device__ __forceinline__ float group_reduce(float v, Op op) {
+  if constexpr (G == 64) return wave_reduce(v, op);
 #pragma unroll
-  for (int s = 0; s < kSlots; ++s) {
-    const int e = lane + s * kWave;
-    p[s] = e < E ? row[e] : -INFINITY;
-    top = fmaxf(top, p[s]);
-  }
-  top = wave_max(top);
+  for (int d = G / 2; d >= 1; d /= 2) v = op(v, __shfl_xor(v, d));
+  return v;
+}
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+  return group_reduce<G>(v, [](float a, float b) { return a + b; });
+}
+
+// p: the token's logits on entry (-inf past E), its softmax on return; returns log sum exp.
+template <int G, int S>
+__device__ __forceinline__ float group_softmax(float (&p)[S]) {
+  float top = p[0];
+#pragma unroll
+  for (int s = 1; s < S; ++s) top = fmaxf(top, p[s]);
+  top = group_reduce<G>(top, [](float a, float b) { return fmaxf(a, b); });
   float sum = 0.f;
 #pragma unroll
-  for (int s = 0; s < kSlots; ++s) {
-    p[s] = lane + s * kWave < E ? expf(p[s] - top) : 0.f;
+  for (int s = 0; s < S; ++s) {
+    p[s] = expf(p[s] - top);
     sum += p[s];
   }
-  sum = wave_sum(sum);
+  sum = group_sum<G>(sum);
+  const float inv = 1.f / sum;
 #pragma unroll
-  for (int s = 0; s < kSlots; ++s) p[s] /= sum;
+  for (int s = 0; s < S; ++s) p[s] *= inv;
   return top + logf(sum);
 }
 
-__global__ __launch_bounds__(kThreads) void balance_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
-                                                           const uint8_t* __restrict__ mask, int T, int E, int k,
-                                                           int32_t* __restrict__ counts, float* __restrict__ mean_prob,
-                                                           float* __restrict__ losses) {
-  __shared__ int32_t cnt[MOE_MAX_EXPERTS + 1];
-  __shared__ float prob[kWaves][MOE_MAX_EXPERTS], zsum[kWaves], part[kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int e = tid; e <= E; e += kThreads) cnt[e] = 0;
-  __syncthreads();
-  float mine[kSlots] = {}, z = 0.f;
-  for (int t = wave; t < T; t += kWaves) {
-    if (mask != nullptr && mask[t] == 0) continue;
-    float p[kSlots];
-    const float lse = row_softmax(logits + (size_t)t * E, lane, E, p);
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s) mine[s] += p[s];
-    z = fmaf(lse, lse, z);
-    if (lane < k) {
-      const int e = idx[(size_t)t * k + lane];
-      if ((unsigned)e < (unsigned)E) atomicAdd(&cnt[e], 1);
-    }
-    if (lane == 0) atomicAdd(&cnt[E], 1);
-  }
-#pragma unroll
-  for (int s = 0; s < kSlots; ++s) prob[wave][lane + s * kWave] = mine[s];
-  if (lane == 0) zsum[wave] = z;
-  __syncthreads();
+// ---- balance loss ----------------------------------------------------------------------------------------------------------
+// A workgroup takes every gridDim.x-th run of tokens and leaves the sums of its probabilities, squared logarithms and counts; the
+// counts are integers added in LDS, whose order does not matter, the rest is added in a fixed order.  One workgroup alone finishes by
+// itself, several leave their sums to balance_join_kernel.
+constexpr int kLossThreads = 512, kLossWaves = kLossThreads / kWave;
+
+struct Balance {
+  const float* logits;
+  const int32_t* idx;
+  const uint8_t* mask;
+  int T, E, k;
+  int32_t* counts;    // [E+1]
+  float* mean_prob;   // [E]
+  float* losses;      // [2]
+  float* part_prob;   // [workgroups][E+1]: sums of p, of lse^2
+  int32_t* part_cnt;  // [workgroups][E+1]
+};
+
+// cnt, prob: totals in LDS, [E] of prob being the sum of squares.
+__device__ __forceinline__ void balance_finish(const Balance& b, const int32_t* cnt, const float* prob, float* s_red) {
+  const int tid = threadIdx.x, E = b.E;
   const float many = fmaxf((float)cnt[E], 1.f);
-  float b = 0.f;
-  if (tid <= E) counts[tid] = cnt[tid];
-  if (tid == 0) counts[E] = cnt[E];
-  if (tid < E) {
-    float sum = 0.f;
-    for (int w = 0; w < kWaves; ++w) sum += prob[w][tid];
-    mean_prob[tid] = sum / many;
-    b = sum / many * ((float)cnt[tid] / many);
+  float sum = 0.f;
+  for (int e = tid; e <= E; e += kLossThreads) {
+    b.counts[e] = cnt[e];
+    if (e < E) {
+      const float mean = prob[e] / many;
+      b.mean_prob[e] = mean;
+      sum = fmaf(mean, (float)cnt[e] / many, sum);
+    }
   }
-  b = wave_sum(b);
-  if (lane == 0) part[wave] = b;
+  sum = wave_sum(sum);
+  if ((tid & 63) == 0) s_red[tid >> 6] = sum;
   __syncthreads();
   if (tid == 0) {
-    float sum = 0.f, zs = 0.f;
-    for (int w = 0; w < kWaves; ++w) sum += part[w], zs += zsum[w];
-    losses[0] = sum * ((float)E / k);
-    losses[1] = zs / many;
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kLossWaves; ++w) total += s_red[w];
+    b.losses[0] = total * ((float)E / b.k);
+    b.losses[1] = prob[E] / many;
   }
 }
 
-// a wavefront per token
-__global__ __launch_bounds__(kThreads) void route_backward_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
-                                                                  const float* __restrict__ d_topk_w,
-                                                                  const uint8_t* __restrict__ mask,
-                                                                  const int32_t* __restrict__ counts, int T, int E, int k,
-                                                                  float coef_balance, float coef_z, bool renorm,
-                                                                  float* __restrict__ d_logits) {
-  const int lane = threadIdx.x & 63, t = blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (t >= T) return;
-  const bool counts_in = mask == nullptr || mask[t] != 0;
-  float d[kSlots] = {};
-  if (counts_in || d_topk_w != nullptr) {
-    float p[kSlots];
-    const float lse = row_softmax(logits + (size_t)t * E, lane, E, p);
-    if (d_topk_w != nullptr) {
-      float w[kSlots], dw[kSlots], sum = 0.f;
+template <int G, int S>
+__global__ __launch_bounds__(kLossThreads) void balance_kernel(Balance b) {
+  constexpr int kGroups = kLossThreads / G;
+  __shared__ int32_t cnt[MOE_MAX_EXPERTS + 1];
+  __shared__ float sums[kGroups][G * S], zsum[kGroups], total[MOE_MAX_EXPERTS + 1], red[kLossWaves];
+  const int tid = threadIdx.x, l = tid & (G - 1), group = tid / G, E = b.E;
+  for (int e = tid; e <= E; e += kLossThreads) cnt[e] = 0;
+  __syncthreads();
+  float mine[S], z = 0.f;
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s) {
-        dw[s] = 0.f;
-        bool picked = false;
-        for (int j = 0; j < k; ++j)
-          if (idx[(size_t)t * k + j] == lane + s * kWave) picked = true, dw[s] += d_topk_w[(size_t)t * k + j];
-        w[s] = renorm && !picked ? 0.f : p[s];
-        sum += w[s];
-      }
-      sum = renorm ? wave_sum(sum) : 1.f;
-      float dot = 0.f;
+  for (int s = 0; s < S; ++s) mine[s] = 0.f;
+  const int step = gridDim.x * kGroups;
+  for (int t = blockIdx.x * kGroups + group; t < b.T; t += step) {
+    if (b.mask != nullptr && b.mask[t] == 0) continue;
+    float p[S];
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s) w[s] /= sum, dot = fmaf(w[s], dw[s], dot);
-      dot = wave_sum(dot);
-#pragma unroll
-      for (int s = 0; s < kSlots; ++s) d[s] = w[s] * (dw[s] - dot);
+    for (int s = 0; s < S; ++s) p[s] = l + G * s < E ? b.logits[(size_t)t * E + l + G * s] : -INFINITY;
+    for (int j = l; j < b.k; j += G) {
+      const int e = b.idx[(size_t)t * b.k + j];
+      if ((unsigned)e < (unsigned)E) atomicAdd(&cnt[e], 1);
     }
-    if (counts_in && counts != nullptr) {
-      const float many = fmaxf((float)counts[E], 1.f), even = (float)k * many / (float)E;
-      const float c = coef_balance * E / k / many / many, cz = 2.f * coef_z / many * lse;
-      float g[kSlots], dot = 0.f;
+    if (l == 0) atomicAdd(&cnt[E], 1);
+    const float lse = group_softmax<G, S>(p);
+    z = fmaf(lse, lse, z);
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s) {
-        const int e = lane + s * kWave;
-        g[s] = e < E ? c * ((float)counts[e] - even) : 0.f;  // (the gradient is the same with any constant taken off)
+    for (int s = 0; s < S; ++s) mine[s] += p[s];
+  }
+#pragma unroll
+  for (int s = 0; s < S; ++s) sums[group][l + G * s] = mine[s];
+  if (l == 0) zsum[group] = z;
+  __syncthreads();
+  for (int e = tid; e <= E; e += kLossThreads) {
+    float sum = 0.f;
+    for (int g = 0; g < kGroups; ++g) sum += e < E ? sums[g][e] : zsum[g];
+    total[e] = sum;
+  }
+  __syncthreads();
+  if (gridDim.x == 1) return balance_finish(b, cnt, total, red);
+  for (int e = tid; e <= E; e += kLossThreads) {
+    b.part_prob[(size_t)blockIdx.x * (E + 1) + e] = total[e];
+    b.part_cnt[(size_t)blockIdx.x * (E + 1) + e] = cnt[e];
+  }
+}
+
+__global__ __launch_bounds__(kLossThreads) void balance_join_kernel(Balance b, int parts) {
+  __shared__ int32_t cnt[MOE_MAX_EXPERTS + 1], s_cnt[kLossWaves][kWave];
+  __shared__ float total[MOE_MAX_EXPERTS + 1], s_sum[kLossWaves][kWave], red[kLossWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, E1 = b.E + 1;
+  for (int e0 = 0; e0 < E1; e0 += kWave) {  // 64 columns at a time, a share of the parts a wavefront
+    const int e = e0 + lane;
+    float sum = 0.f;
+    int c = 0;
+    if (e < E1)
+#pragma unroll 8
+      for (int p = wave; p < parts; p += kLossWaves) {
+        sum += b.part_prob[(size_t)p * E1 + e];
+        c += b.part_cnt[(size_t)p * E1 + e];
+      }
+    s_sum[wave][lane] = sum;
+    s_cnt[wave][lane] = c;
+    __syncthreads();
+    if (wave == 0 && e < E1) {
+      float all = 0.f;
+      int n = 0;
+#pragma unroll
+      for (int w = 0; w < kLossWaves; ++w) all += s_sum[w][lane], n += s_cnt[w][lane];
+      total[e] = all;
+      cnt[e] = n;
+    }
+    __syncthreads();
+  }
+  balance_finish(b, cnt, total, red);
+}
+
+// ---- gradient of the logits ------------------------------------------------------------------------------------------------
+struct RouteBackward {
+  const float *logits, *d_topk_w;
+  const int32_t *idx, *counts;
+  const uint8_t* mask;
+  int T, E, k;
+  float coef_balance, coef_z;
+  bool renorm;
+  float* d_logits;
+};
+
+template <int G, int S>
+__global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward b) {
+  const int l = threadIdx.x & (G - 1), E = b.E, k = b.k;
+  const int t = blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  if (t >= b.T) return;
+  const bool counted = b.counts != nullptr && (b.mask == nullptr || b.mask[t] != 0);
+  float d[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) d[s] = 0.f;
+  if (counted || b.d_topk_w != nullptr) {
+    float p[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) p[s] = l + G * s < E ? b.logits[(size_t)t * E + l + G * s] : -INFINITY;
+    const float lse = group_softmax<G, S>(p);
+    if (b.d_topk_w != nullptr) {
+      // gates: the softmax over all experts, or over the picked ones alone; dw: the gradient at each picked expert
+      float w[S], dw[S], sum = 0.f, dot = 0.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) w[s] = b.renorm ? 0.f : p[s], dw[s] = 0.f;
+      for (int j = 0; j < k; ++j) {
+        const int e = b.idx[(size_t)t * k + j];
+        const float g = b.d_topk_w[(size_t)t * k + j];
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+          if (e == l + G * s) w[s] = p[s], dw[s] = g;
+      }
+#pragma unroll
+      for (int s = 0; s < S; ++s) sum += w[s];
+      const float inv = b.renorm ? 1.f / group_sum<G>(sum) : 1.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) w[s] *= inv, dot = fmaf(w[s], dw[s], dot);
+      dot = group_sum<G>(dot);
+#pragma unroll
+      for (int s = 0; s < S; ++s) d[s] = w[s] * (dw[s] - dot);
+    }
+    if (counted) {
+      // the load's gradient is the same with a constant taken off: off the even load, which leaves small numbers to subtract
+      const float many = fmaxf((float)b.counts[E], 1.f), even = (float)k * many / (float)E;
+      const float c = b.coef_balance * (float)E / ((float)k * many * many), cz = 2.f * b.coef_z / many * lse;
+      float g[S], dot = 0.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        g[s] = l + G * s < E ? c * ((float)b.counts[l + G * s] - even) : 0.f;
         dot = fmaf(p[s], g[s], dot);
       }
-      dot = wave_sum(dot);
+      dot = group_sum<G>(dot);
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s) d[s] += p[s] * (g[s] - dot + cz);
+      for (int s = 0; s < S; ++s) d[s] += p[s] * (g[s] - dot + cz);
     }
   }
 #pragma unroll
-  for (int s = 0; s < kSlots; ++s)
-    if (lane + s * kWave < E) d_logits[(size_t)t * E + lane + s * kWave] = d[s];
+  for (int s = 0; s < S; ++s)
+    if (l + G * s < E) b.d_logits[(size_t)t * E + l + G * s] = d[s];
 }
 
-__global__ __launch_bounds__(kThreads) void router_weight_grad_kernel(const uint16_t* __restrict__ x,
-                                                                      const float* __restrict__ d_logits, int T, int H, int E,
-                                                                      float* __restrict__ d_w) {
-  const int e = blockIdx.x, h = blockIdx.y * kThreads + threadIdx.x;
-  if (h >= H) return;
-  float sum = 0.f;
-  for (int t = 0; t < T; ++t) sum = fmaf(bf16_bits_to_f32(x[(size_t)t * H + h]), d_logits[(size_t)t * E + e], sum);
-  d_w[(size_t)h * E + e] = sum;
+// One kernel for each number of lanes a token needs.
+template <template <int, int> class Launch, typename... Args>
+void by_width(int E, Args... args) {
+  if (E <= 8) Launch<8, 1>::run(args...);
+  else if (E <= 16) Launch<16, 1>::run(args...);
+  else if (E <= 32) Launch<32, 1>::run(args...);
+  else if (E <= 64) Launch<64, 1>::run(args...);
+  else if (E <= 128) Launch<64, 2>::run(args...);
+  else Launch<64, 4>::run(args...);
 }
 
-__global__ __launch_bounds__(kThreads) void router_input_grad_kernel(const float* __restrict__ w_router,
-                                                                     const float* __restrict__ d_logits, int H, int E,
-                                                                     const uint16_t* dx_in, uint16_t* dx) {
-  const int t = blockIdx.x, h = blockIdx.y * kThreads + threadIdx.x;
-  if (h >= H) return;
-  float sum = 0.f;
-  for (int e = 0; e < E; ++e) sum = fmaf(d_logits[(size_t)t * E + e], w_router[(size_t)h * E + e], sum);
-  if (dx_in != nullptr) sum += bf16_bits_to_f32(dx_in[(size_t)t * H + h]);
-  dx[(size_t)t * H + h] = (uint16_t)f32_to_bf16_bits(sum);
+// About 64 tokens a wavefront's worth of work, at most two workgroups a compute unit.
+int loss_workgroups(int T, int E) {
+  const int lanes = E <= 8 ? 8 : (E <= 16 ? 16 : (E <= 32 ? 32 : 64));
+  const int n = ceil_div(T, 4 * (kLossThreads / lanes));
+  return n < 1 ? 1 : (n > 512 ? 512 : n);
 }
 
-__device__ __forceinline__ float at(const float* p, size_t i) { return p[i]; }
-__device__ __forceinline__ float at(const uint16_t* p, size_t i) { return bf16_bits_to_f32(p[i]); }
+template <int G, int S>
+struct LaunchBalance {
+  static void run(const Balance& b, int groups, hipStream_t s) {
+    hipLaunchKernelGGL((balance_kernel<G, S>), dim3(groups), dim3(kLossThreads), 0, s, b);
+  }
+};
+template <int G, int S>
+struct LaunchRoute {
+  static void run(const RouteBackward& b, hipStream_t s) {
+    hipLaunchKernelGGL((route_backward_kernel<G, S>), dim3(ceil_div(b.T, kThreads / G)), dim3(kThreads), 0, s, b);
+  }
+};
 
-// a wavefront per (token, slot); slot k is the shared expert's gate
-template <typename YT>
+// ---- gradient of the router's product --------------------------------------------------------------------------------------
+// d_w_router is the outer product of skinny.hpp over all rows, dx its expansion, with W_r in two bf16 parts: rows [h][part][R] of R =
+// 32, 64, 128 or 256 columns, zeros past E.
+int router_width(int E) { return E <= 32 ? 32 : (E <= 64 ? 64 : (E <= 128 ? 128 : 256)); }
+
+__global__ __launch_bounds__(kThreads) void split_router_kernel(const float* __restrict__ w, int64_t n, int E, int R,
+                                                                uint16_t* __restrict__ out) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t h = i / R;
+    const int e = (int)(i - h * R);
+    const float v = e < E ? w[h * E + e] : 0.f;
+    const uint32_t hi = f32_to_bf16_bits(v);
+    out[h * 2 * R + e] = (uint16_t)hi;
+    out[h * 2 * R + R + e] = (uint16_t)f32_to_bf16_bits(v - bf16_bits_to_f32(hi));
+  }
+}
+
+struct RouterPlan {
+  int chunk, pieces, slots;
+  size_t split, outer, bytes;  // offsets in the workspace
+};
+RouterPlan plan_router(int T, int H, int E) {
+  RouterPlan p = {};
+  const int tiles = ceil_div(H, kOuterCols) * ceil_div(E, 64);
+  const int chunk = (int)(((int64_t)T * tiles / 256 + 255) / 256 * 256);  // about 256 workgroups, of 256 rows at least
+  p.chunk = chunk < 256 ? 256 : chunk;
+  p.pieces = T > p.chunk ? ceil_div(T, p.chunk) : 1;
+  p.slots = T > p.chunk ? p.pieces : 0;
+  p.split = 0;
+  p.outer = padded((size_t)H * 2 * router_width(E) * 2);
+  p.bytes = p.outer + padded((size_t)p.slots * H * E * sizeof(float));
+  return p;
+}
+
+template <int WCH, int NJ>
+void launch_router_expand(Expand e, hipStream_t s) {
+  constexpr int M = 2 * 32 * WCH <= 256 ? 128 : 64;  // as in the kernel
+  e.n_tiles = ceil_div(e.rows.T, M);
+  hipLaunchKernelGGL((expand_kernel<uint16_t, 2, WCH, NJ, true>), dim3(ceil_div(e.N, kExpandWaves * 16 * NJ), e.n_tiles),
+                     dim3(kExpandThreads), 0, s, e);
+}
+
+// ---- gradient of the combine's gates ---------------------------------------------------------------------------------------
+// A workgroup per token: every lane holds 8 columns of dy and meets the token's rows of y one after the other, so dy is read once and
+// each row of y once, 16 or 32 bytes a lane; the k + 1 sums are joined at the end.  Bound by y's bytes.
+template <typename YT, int KMAX>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const uint16_t* __restrict__ dy, const YT* __restrict__ y_perm,
-                                                                    const int32_t* __restrict__ slot_row, int T, int k, int H,
+                                                                    const int32_t* __restrict__ slot_row, int k, int H,
                                                                     const YT* __restrict__ y_shared,
                                                                     const uint16_t* __restrict__ x,
                                                                     const float* __restrict__ w_shared_gate,
                                                                     float* __restrict__ d_topk_w,
                                                                     float* __restrict__ d_shared_gate) {
-  const int t = blockIdx.x, lane = threadIdx.x & 63;
-  for (int j = threadIdx.x >> 6; j < k + (y_shared != nullptr); j += kWaves) {
-    const int row = j < k ? slot_row[(size_t)t * k + j] : t;
-    const YT* y = j < k ? y_perm : y_shared;
-    float sum = 0.f, z = 0.f;
-    if (row >= 0)
-      for (int h = lane; h < H; h += kWave) {
-        sum = fmaf(at(dy, (size_t)t * H + h), at(y, (size_t)row * H + h), sum);
-        if (j == k) z = fmaf(at(x, (size_t)t * H + h), w_shared_gate[h], z);
+  __shared__ float red[kWaves][KMAX + 2];
+  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  float acc[KMAX], shared = 0.f, z = 0.f;
+  int row[KMAX];
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j) {
+    acc[j] = 0.f;
+    row[j] = j < k ? slot_row[(size_t)t * k + j] : -1;
+  }
+  for (int h = tid * 8; h < H; h += kThreads * 8) {
+    float g[8], v[8];
+    load8(dy + (size_t)t * H + h, g);
+#pragma unroll
+    for (int j = 0; j < KMAX; ++j)
+      if (row[j] >= 0) {
+        load8(y_perm + (size_t)row[j] * H + h, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[j] = fmaf(g[i], v[i], acc[j]);
       }
-    sum = wave_sum(sum);
-    if (j < k) {
-      if (lane == 0) d_topk_w[(size_t)t * k + j] = sum;
-    } else {
-      const float gate = 1.f / (1.f + expf(-wave_sum(z)));
-      if (lane == 0) d_shared_gate[t] = gate * (1.f - gate) * sum;
+    if (y_shared != nullptr) {
+      load8(y_shared + (size_t)t * H + h, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) shared = fmaf(g[i], v[i], shared);
+      float w[8];
+      load8(x + (size_t)t * H + h, v);
+      load8(w_shared_gate + h, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z = fmaf(v[i], w[i], z);
     }
   }
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j) {
+    const float sum = wave_sum(acc[j]);
+    if (lane == 0) red[wave][j] = sum;
+  }
+  if (y_shared != nullptr) {
+    shared = wave_sum(shared);
+    z = wave_sum(z);
+    if (lane == 0) red[wave][KMAX] = shared, red[wave][KMAX + 1] = z;
+  }
+  __syncthreads();
+  if (tid < k) {
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += red[w][tid];
+    d_topk_w[(size_t)t * k + tid] = sum;
+  }
+  if (tid == 64 && y_shared != nullptr) {
+    float sum = 0.f, logit = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += red[w][KMAX], logit += red[w][KMAX + 1];
+    const float gate = 1.f / (1.f + expf(-logit));
+    d_shared_gate[t] = gate * (1.f - gate) * sum;
+  }
+}
+
+template <typename YT>
+void launch_combine_backward(const uint16_t* dy, const void* y_perm, const int32_t* slot_row, int T, int k, int H,
+                             const void* y_shared, const uint16_t* x, const float* w, float* d_topk_w, float* d_gate,
+                             hipStream_t s) {
+  const auto kernel = k <= 1   ? combine_backward_kernel<YT, 1>
+                      : k <= 2 ? combine_backward_kernel<YT, 2>
+                      : k <= 4 ? combine_backward_kernel<YT, 4>
+                      : k <= 8 ? combine_backward_kernel<YT, 8>
+                               : combine_backward_kernel<YT, 16>;
+  hipLaunchKernelGGL(kernel, dim3(T), dim3(kThreads), 0, s, dy, static_cast<const YT*>(y_perm), slot_row, k, H,
+                     static_cast<const YT*>(y_shared), x, w, d_topk_w, d_gate);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -201,15 +400,15 @@ int router_status(int32_t T, int32_t H, int32_t E) {
   return H % 8 != 0 ? MOE_ERR_UNSUPPORTED_SHAPE : MOE_OK;
 }
 
-int blocks(int n) { return (n + kThreads - 1) / kThreads; }
-
 }  // namespace
 }  // namespace moe
 
 extern "C" {
 
 size_t moe_balance_workspace_bytes(int32_t T, int32_t E) {
-  return moe::losses_status(T, E, 1) == MOE_OK ? 256 : 0;
+  using namespace moe;
+  if (losses_status(T, E, 1) != MOE_OK) return 0;
+  return 2 * padded((size_t)loss_workgroups(T, E) * (E + 1) * 4);
 }
 
 int moe_balance_loss(const float* logits, const int32_t* topk_idx, const uint8_t* token_mask, int32_t T, int32_t E, int32_t k,
@@ -220,8 +419,12 @@ int moe_balance_loss(const float* logits, const int32_t* topk_idx, const uint8_t
   if (T > 0 && (logits == nullptr || topk_idx == nullptr)) return MOE_ERR_INVALID_ARG;
   if (counts == nullptr || mean_prob == nullptr || losses == nullptr) return MOE_ERR_INVALID_ARG;
   if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < moe_balance_workspace_bytes(T, E)) return MOE_ERR_WORKSPACE;
-  hipLaunchKernelGGL(balance_kernel, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), logits, topk_idx, token_mask, T,
-                     E, k, counts, mean_prob, losses);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int groups = loss_workgroups(T, E);
+  const Balance b{logits, topk_idx, token_mask, T, E, k, counts, mean_prob, losses, static_cast<float*>(workspace),
+                  reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + padded((size_t)groups * (E + 1) * 4))};
+  by_width<LaunchBalance>(E, b, groups, s);
+  if (groups > 1) hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(kLossThreads), 0, s, b, groups);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -236,14 +439,14 @@ int moe_route_backward(const float* logits, const int32_t* topk_idx, const float
   if (!std::isfinite(coef_balance) || !std::isfinite(coef_z)) return MOE_ERR_INVALID_ARG;
   if (counts == nullptr && (coef_balance != 0.f || coef_z != 0.f)) return MOE_ERR_INVALID_ARG;
   if (T == 0) return MOE_OK;
-  hipLaunchKernelGGL(route_backward_kernel, dim3((T + kWaves - 1) / kWaves), dim3(kThreads), 0, static_cast<hipStream_t>(stream),
-                     logits, topk_idx, d_topk_w, token_mask, counts, T, E, k, coef_balance, coef_z,
-                     (flags & MOE_RENORM_TOPK) != 0, d_logits);
+  const RouteBackward b{logits, d_topk_w, topk_idx, counts, token_mask, T, E, k, coef_balance, coef_z,
+                        (flags & MOE_RENORM_TOPK) != 0, d_logits};
+  by_width<LaunchRoute>(E, b, static_cast<hipStream_t>(stream));
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
 size_t moe_router_backward_workspace_bytes(int32_t T, int32_t H, int32_t E) {
-  return moe::router_status(T, H, E) == MOE_OK ? 256 : 0;
+  return moe::router_status(T, H, E) == MOE_OK ? moe::plan_router(T, H, E).bytes : 0;
 }
 
 int moe_router_backward(const void* x_bf16, const float* w_router, const float* d_logits, int32_t T, int32_t H, int32_t E,
@@ -253,15 +456,34 @@ int moe_router_backward(const void* x_bf16, const float* w_router, const float* 
   if (st != MOE_OK) return st;
   if (T > 0 && (x_bf16 == nullptr || d_logits == nullptr)) return MOE_ERR_INVALID_ARG;
   if (d_w_router == nullptr || (dx == nullptr ? dx_in != nullptr : w_router == nullptr)) return MOE_ERR_INVALID_ARG;
-  if (!aligned16(x_bf16) || !aligned16(dx_in) || !aligned16(dx)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(x_bf16) || !aligned16(dx_in) || !aligned16(dx) || !aligned16(d_w_router)) return MOE_ERR_INVALID_ARG;
   if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < moe_router_backward_workspace_bytes(T, H, E))
     return MOE_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(router_weight_grad_kernel, dim3(E, blocks(H)), dim3(kThreads), 0, s, static_cast<const uint16_t*>(x_bf16),
-                     d_logits, T, H, E, d_w_router);
-  if (dx != nullptr && T > 0)
-    hipLaunchKernelGGL(router_input_grad_kernel, dim3(T, blocks(H)), dim3(kThreads), 0, s, w_router, d_logits, H, E,
-                       static_cast<const uint16_t*>(dx_in), static_cast<uint16_t*>(dx));
+  const RouterPlan p = plan_router(T, H, E);
+  char* const ws = static_cast<char*>(workspace);
+  const Rows rows{nullptr, nullptr, nullptr, T, 1};
+  const Outer o{rows,
+                {{static_cast<const uint16_t*>(x_bf16), d_logits, nullptr, d_w_router, reinterpret_cast<float*>(ws + p.outer), H,
+                  ceil_div(H, kOuterCols), true},
+                 {}},
+                E, p.chunk};
+  const dim3 block(kOuterWaves * 64);
+  if (E <= 16) hipLaunchKernelGGL(outer_kernel<1>, dim3(o.side[0].tiles, p.pieces, 1), block, 0, s, o);
+  else if (E <= 32) hipLaunchKernelGGL(outer_kernel<2>, dim3(o.side[0].tiles, p.pieces, 1), block, 0, s, o);
+  else hipLaunchKernelGGL(outer_kernel<4>, dim3(o.side[0].tiles, p.pieces, ceil_div(E, 64)), block, 0, s, o);
+  if (p.slots > 0) hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div((int64_t)E * H, 4096), 1), dim3(256), 0, s, o);
+  if (dx != nullptr && T > 0) {
+    const int R = router_width(E);
+    uint16_t* const split = reinterpret_cast<uint16_t*>(ws + p.split);
+    hipLaunchKernelGGL(split_router_kernel, dim3(ceil_div((int64_t)H * R, 4 * kThreads)), dim3(kThreads), 0, s, w_router,
+                       (int64_t)H * R, E, R, split);
+    const Expand e{rows, d_logits, 1, E, nullptr, nullptr, false, split, 2 * R, H, dx_in, dx, 0, E % 4 == 0 && aligned16(d_logits)};
+    if (R == 32) launch_router_expand<1, 4>(e, s);
+    else if (R == 64) launch_router_expand<2, 4>(e, s);
+    else if (R == 128) launch_router_expand<4, 2>(e, s);
+    else launch_router_expand<8, 2>(e, s);
+  }
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -284,11 +506,9 @@ int moe_combine_backward(const void* dy_bf16, const void* y_perm, const int32_t*
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const uint16_t *dy = static_cast<const uint16_t*>(dy_bf16), *x = static_cast<const uint16_t*>(x_bf16);
   if (flags & MOE_Y_PERM_BF16)
-    hipLaunchKernelGGL(combine_backward_kernel<uint16_t>, dim3(T), dim3(kThreads), 0, s, dy, static_cast<const uint16_t*>(y_perm),
-                       slot_row, T, k, H, static_cast<const uint16_t*>(y_shared), x, w_shared_gate, d_topk_w, d_shared_gate);
+    launch_combine_backward<uint16_t>(dy, y_perm, slot_row, T, k, H, y_shared, x, w_shared_gate, d_topk_w, d_shared_gate, s);
   else
-    hipLaunchKernelGGL(combine_backward_kernel<float>, dim3(T), dim3(kThreads), 0, s, dy, static_cast<const float*>(y_perm),
-                       slot_row, T, k, H, static_cast<const float*>(y_shared), x, w_shared_gate, d_topk_w, d_shared_gate);
+    launch_combine_backward<float>(dy, y_perm, slot_row, T, k, H, y_shared, x, w_shared_gate, d_topk_w, d_shared_gate, s);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

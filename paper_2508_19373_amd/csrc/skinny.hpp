@@ -484,7 +484,7 @@ __global__ __launch_bounds__(kOuterWaves * 64) void outer_kernel(Outer o) {
 }
 
 // Adds the pieces of cut groups in order.  blockIdx.y: the group.
-__global__ __launch_bounds__(256) void reduce_kernel(Outer o) {
+static __global__ __launch_bounds__(256) void reduce_kernel(Outer o) {
   const int g = blockIdx.y;
   const int first = o.rows.offsets != nullptr ? o.rows.offsets[g] : 0;
   const int n = o.rows.offsets != nullptr ? o.rows.offsets[g + 1] - first : o.rows.T;

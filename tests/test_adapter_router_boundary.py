@@ -100,7 +100,7 @@ def test_router_and_combine_backward_refusals(lib):
     invalid, shape = B.MOE_ERR_INVALID_ARG, B.MOE_ERR_UNSUPPORTED_SHAPE
     f = lib.moe_router_backward
     for change in (dict(T=-1), dict(T=1 << 24), dict(H=0), dict(E=0), dict(E=257), dict(x=None), dict(dl=None), dict(dw=None),
-                   dict(w=None), dict(dx=None), dict(x=P + 8), dict(dx=P + 8), dict(dx_in=P + 8)):
+                   dict(w=None), dict(dx=None), dict(x=P + 8), dict(dw=P + 8), dict(dx=P + 8), dict(dx_in=P + 8)):
         assert _call(f, ROUTER, **change) == invalid, change
     assert _call(f, ROUTER, H=60) == shape
     need = B.moe_router_backward_workspace_bytes(4, 64, 8)
