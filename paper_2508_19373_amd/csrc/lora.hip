@@ -1,11 +1,10 @@
 // Low-rank adapters of many requests beside one projection: y += scale_a (x A_a^T) B_a^T with the row's own adapter a, and the
 // gradients of A, B and x.
 //
-// Rows are first sorted by adapter (moe_permute's index kernels; not up to 64 rows, where a wavefront sees all ids at once), then
+// A decoding batch of up to 64 rows: shrink_few_kernel, expand_few_kernel.  More rows are sorted by adapter first (skinny.hpp):
 //   forward:  v = shrink(x, A), y = expand(v, B)
 //   backward: u = shrink(dy, B^T), dx = expand(u, A^T), grad A = outer(u, x), grad B = outer(v, dy)
-// with the kernels of skinny.hpp.  B^T and A^T are written out first: a few MB, where the products read them 16 bytes at a time along the
-// side that is summed.
+// B^T and A^T are written out for that: a few MB, where the products read them 16 bytes at a time along the side that is summed.
 #include "moe_lora.h"
 #include "skinny.hpp"
 
@@ -14,29 +13,244 @@ namespace {
 
 using namespace skinny;
 
-// out[c][r] = in[r][c] for each adapter that has rows; A in the first tiles_a tiles of 64 x 64, B behind them.
-struct Transpose {
+// ---- up to 64 rows -------------------------------------------------------------------------------------------------------------
+// Two short kernels, bound by their latency: every workgroup looks at all ids, one a lane.  The first row of an adapter stands for all of its
+// rows, sixteen at a time; the workgroups of the others end at once.  The adapters' matrices are read straight into the MFMA's operands
+// (through LDS, as for many rows, took 7.5 and 7.2 us instead of 5.7 and 5.0 with 48 rows of 32 adapters, 4096 x 4096, rank 16).
+constexpr int kFewRows = 64, kFewTile = 16;
+
+struct Few {
+  const int32_t* idx;
+  int T, L;
+};
+
+// Rows of workgroup b = leader * ceil(T / 16) + part: fills s_rows, returns how many; group -1: without an adapter.
+__device__ __forceinline__ int few_rows(const Few& f, int b, int32_t* s_rows, int& group) {
+  const int lane = threadIdx.x & (kWave - 1), parts = (f.T + kFewTile - 1) / kFewTile, leader = b / parts, first = b % parts * kFewTile;
+  int g = lane < f.T ? f.idx[lane] : -2;
+  if (lane < f.T && (unsigned)g >= (unsigned)f.L) g = -1;
+  group = (int)__builtin_amdgcn_readlane(g, leader);
+  const unsigned long long same = __ballot(g == group);
+  const int n = min((int)__popcll(same) - first, kFewTile);
+  if (__ffsll((long long)same) - 1 != leader || n <= 0) return 0;
+  const int rank = (int)__popcll(same & ((1ull << lane) - 1ull)) - first;
+  if (threadIdx.x < kWave && g == group && rank >= 0 && rank < kFewTile) s_rows[rank] = lane;
+  return n;
+}
+
+constexpr int kFewWaves = 8;
+
+// blockIdx.y: a piece of the sum over k; part [pieces][T][r].  A wavefront multiplies the rows by all of A_a over every
+// (8 gridDim.y)-th 64 of k; lane (row, q) loads k = 16 q .. 16 q + 15 of them and so does the lane of A_a, whose halves the two MFMAs take.
+template <int NT>
+__global__ __launch_bounds__(kFewWaves * 64) void shrink_few_kernel(Few few, const uint16_t* __restrict__ x, int K,
+                                                                    const uint16_t* __restrict__ m, int r, float* __restrict__ part) {
+  __shared__ int32_t s_rows[kFewTile];
+  __shared__ float red[kFewWaves][16][NT * 16 + 1];
+  int group;
+  const int n = few_rows(few, blockIdx.x, s_rows, group);
+  if (n == 0 || group < 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = lane & 15, q = lane >> 4;
+  const uint16_t* mr[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) mr[j] = m + ((size_t)group * r + min(16 * j + row, r - 1)) * K + 16 * q;
+  __syncthreads();
+  const uint16_t* const xr = x + (size_t)s_rows[min(row, n - 1)] * K + 16 * q;
+  f32x4 acc[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int stride = kFewWaves * gridDim.y * 64;
+  for (int c = (blockIdx.y * kFewWaves + wave) * 64; c < K; c += stride) {
+    u32x4 xv[2], mv[NT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool in = c + 8 * h + 16 * q < K;  // (K is a multiple of 8)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) mv[j][h] = in ? *reinterpret_cast<const u32x4*>(mr[j] + c + 8 * h) : u32x4{};
+      xv[h] = in ? *reinterpret_cast<const u32x4*>(xr + c + 8 * h) : u32x4{};
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[j] = mfma(xv[h], mv[j][h], acc[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[wave][4 * q + e][16 * j + row] = acc[j][e];
+  __syncthreads();
+  part += (size_t)blockIdx.y * few.T * r;
+  for (int o = tid; o < 16 * 16 * NT; o += kFewWaves * 64) {
+    const int ro = o / (16 * NT), col = o % (16 * NT);
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) sum += red[w][ro][col];
+    if (ro < n && col < r) part[(size_t)s_rows[ro] * r + col] = sum;
+  }
+}
+
+// A wavefront computes 64 columns: lane (c, q) holds four neighbouring ones of row c for each accumulator, dealt so that 16 bytes of a row
+// are one lane's.  The pieces of v's sum are added in order, its parts go through LDS (rows 16 bytes longer than a multiple of 32).
+struct ExpandFew {
+  Few few;
+  const float* part;
+  int pieces, r;
+  const float* scale;
+  float* keep;
+  const uint16_t* m;
+  int N;
+  const void* y_in;
+  void* y_out;
+};
+
+template <typename YT, int SPLIT, int CH>
+__global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e) {
+  constexpr int R = 32 * CH, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = SPLIT * R * 2 + 16, ITEMS = kFewTile * (R / 8);
+  __shared__ int32_t s_rows[kFewTile];
+  __shared__ __align__(16) char s_p[kFewTile * kRowBytes];
+  static_assert(ITEMS <= kExpandThreads, "a thread has eight values of v at most");
+  int group;
+  const int n = few_rows(e.few, blockIdx.y, s_rows, group);
+  if (n == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, q = lane >> 4, r = e.r;
+  const int nbase = (blockIdx.x * kExpandWaves + wave) * 64;
+  u32x4 w[CH][4];
+  if (group >= 0 && nbase < e.N)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int col = W == 8 ? (j >> 1) * 32 + (ln >> 2) * 8 + (j & 1) * 4 + (ln & 3) : 16 * j + ln;
+      const uint16_t* const mr = e.m + ((size_t)group * e.N + min(nbase + col, e.N - 1)) * r + 8 * q;
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        w[c][j] = 32 * c + 8 * q < r ? *reinterpret_cast<const u32x4*>(mr + 32 * c) : u32x4{};
+    }
+  __syncthreads();
+  if (group < 0) {
+    copy_rows<YT>(e.y_in, e.y_out, e.keep, r, e.N, s_rows, n, blockIdx.x * kExpandWaves * 64, kExpandWaves * 64);
+    return;
+  }
+  const YT* in = static_cast<const YT*>(e.y_in);
+  YT* out = static_cast<YT*>(e.y_out);
+  const int c0 = nbase + q * W;
+  const size_t at = (size_t)s_rows[min(ln, n - 1)] * e.N + c0;
+  u32x4 y[UNITS];
+#pragma unroll
+  for (int h = 0; h < UNITS; ++h)
+    y[h] = in != nullptr && c0 + h * 4 * W < e.N ? *reinterpret_cast<const u32x4*>(in + at + h * 4 * W) : u32x4{};
+  if (tid < ITEMS) {
+    const int i = tid / (R / 8), j0 = tid % (R / 8) * 8;
+    float v[8] = {};
+    if (i < n && j0 < r) {
+      const size_t row = (size_t)s_rows[i] * r + j0, piece = (size_t)e.few.T * r;
+      for (int s0 = 0; s0 < e.pieces; s0 += 4) {
+        float more[4][8];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          if (s0 + s < e.pieces) load8(e.part + (s0 + s) * piece + row, more[s]);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          if (s0 + s < e.pieces)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += more[s][k];
+      }
+      const float scale = e.scale[group];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (e.keep != nullptr && blockIdx.x == 0) e.keep[row + k] = v[k];
+        v[k] *= scale;
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < SPLIT; ++s) *reinterpret_cast<u32x4*>(s_p + i * kRowBytes + s * R * 2 + j0 * 2) = take_bf16(v);
+  }
+  __syncthreads();
+  f32x4 acc[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int s = SPLIT - 1; s >= 0; --s) {  // the small parts first
+      const u32x4 b = *reinterpret_cast<const u32x4*>(s_p + ln * kRowBytes + s * R * 2 + c * 64 + q * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = mfma(w[c][j], b, acc[j]);
+    }
+  if (ln >= n) return;
+#pragma unroll
+  for (int h = 0; h < UNITS; ++h) {
+    if (c0 + h * 4 * W >= e.N) break;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t d = y[h][i];
+      if constexpr (W == 8) {
+        const f32x4 a = acc[2 * h + i / 2];
+        y[h][i] = pack_bf16x2(bf16_lo(d) + a[2 * (i & 1)], bf16_hi(d) + a[2 * (i & 1) + 1]);
+      } else {
+        y[h][i] = __float_as_uint(__uint_as_float(d) + acc[h][i]);
+      }
+    }
+    *reinterpret_cast<u32x4*>(out + at + h * 4 * W) = y[h];
+  }
+}
+
+int few_groups(int T) { return T * ceil_div(T, kFewTile); }
+// Pieces of the sum over k: 64 of k for each of the eight wavefronts, 16 at most.
+int few_pieces(int K) {
+  const int n = ceil_div(K, 64 * kFewWaves);
+  return n > 16 ? 16 : n;
+}
+
+void launch_shrink_few(const Few& few, const uint16_t* x, int K, const uint16_t* m, int r, float* part, hipStream_t s) {
+  const dim3 grid(few_groups(few.T), few_pieces(K)), block(kFewWaves * 64);
+  if (r <= 16) hipLaunchKernelGGL(shrink_few_kernel<1>, grid, block, 0, s, few, x, K, m, r, part);
+  else if (r <= 32) hipLaunchKernelGGL(shrink_few_kernel<2>, grid, block, 0, s, few, x, K, m, r, part);
+  else if (r <= 64) hipLaunchKernelGGL(shrink_few_kernel<4>, grid, block, 0, s, few, x, K, m, r, part);
+  else hipLaunchKernelGGL(shrink_few_kernel<8>, grid, block, 0, s, few, x, K, m, r, part);
+}
+
+template <typename YT, int SPLIT>
+void launch_expand_few(const ExpandFew& e, hipStream_t s) {
+  const dim3 grid(ceil_div(e.N, kExpandWaves * 64), few_groups(e.few.T)), block(kExpandThreads);
+  if (e.r <= 32) hipLaunchKernelGGL((expand_few_kernel<YT, SPLIT, 1>), grid, block, 0, s, e);
+  else if (e.r <= 64) hipLaunchKernelGGL((expand_few_kernel<YT, SPLIT, 2>), grid, block, 0, s, e);
+  else hipLaunchKernelGGL((expand_few_kernel<YT, SPLIT, 4>), grid, block, 0, s, e);
+}
+
+// ---- sorted rows ---------------------------------------------------------------------------------------------------------------
+template <typename YT, int SPLIT>
+void launch_expand(const Expand& e, int n_tiles, hipStream_t s) {
+  if (e.r <= 32) launch_expand_kernel<YT, SPLIT, 1, 1, 8>(e, n_tiles, s);
+  else if (e.r <= 64) launch_expand_kernel<YT, SPLIT, 1, 2, 8>(e, n_tiles, s);
+  else launch_expand_kernel<YT, SPLIT, 1, 4, SPLIT == 2 ? 8 : 4>(e, n_tiles, s);  // (three parts: fewer columns, for the registers)
+}
+
+// Before the products of a backward pass, in one launch: out[c][r] = in[r][c] for A and B of each adapter that has rows, 64 x 64 values a
+// workgroup, and v's fragments for the outer product, 32 rows a workgroup.
+struct Prepare {
   const uint16_t* in[2];
   uint16_t* out[2];
-  int R[2], C[2], tiles_c[2], tiles_a;
+  int R[2], C[2], tiles_c[2], tiles_a, tiles, L;  // A's tiles come first
   const int32_t* offsets;
+  Pack pack;
 };
-__global__ __launch_bounds__(256) void transpose_kernel(Transpose p) {
+__global__ __launch_bounds__(256) void prepare_kernel(Prepare p) {
   __shared__ uint16_t s[64][66];
-  const int g = blockIdx.y;
+  if (blockIdx.x >= (unsigned)(p.tiles * p.L)) return pack_block(p.pack, blockIdx.x - p.tiles * p.L);
+  const int g = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
   if (p.offsets[g] == p.offsets[g + 1]) return;
-  const int side = blockIdx.x >= (unsigned)p.tiles_a, b = side ? blockIdx.x - p.tiles_a : blockIdx.x;
-  const int R = p.R[side], C = p.C[side], r0 = b / p.tiles_c[side] * 64, c0 = b % p.tiles_c[side] * 64;
-  const uint16_t* in = p.in[side] + (size_t)g * R * C;
-  uint16_t* out = p.out[side] + (size_t)g * R * C;
+  const bool second = tile >= p.tiles_a;
+  const int b = second ? tile - p.tiles_a : tile, R = second ? p.R[1] : p.R[0], C = second ? p.C[1] : p.C[0];
+  const int tc = second ? p.tiles_c[1] : p.tiles_c[0], r0 = b / tc * 64, c0 = b % tc * 64;
+  const uint16_t* in = (second ? p.in[1] : p.in[0]) + (size_t)g * R * C;
+  uint16_t* out = (second ? p.out[1] : p.out[0]) + (size_t)g * R * C;
   const int i = threadIdx.x >> 3, j = (threadIdx.x & 7) * 8;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int r = r0 + i + 32 * h, c = c0 + j;
     if (r < R && c < C) {
-      const uint4 v = *reinterpret_cast<const uint4*>(in + (size_t)r * C + c);
+      const u32x4 v = *reinterpret_cast<const u32x4*>(in + (size_t)r * C + c);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[i + 32 * h][j + k] = (uint16_t)(reinterpret_cast<const uint32_t*>(&v)[k / 2] >> (16 * (k & 1)));
+      for (int k = 0; k < 8; ++k) s[i + 32 * h][j + k] = (uint16_t)(v[k / 2] >> (16 * (k & 1)));
     }
   }
   __syncthreads();
@@ -47,123 +261,70 @@ __global__ __launch_bounds__(256) void transpose_kernel(Transpose p) {
       uint32_t v[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = s[j + 2 * k][i + 32 * h] | (uint32_t)s[j + 2 * k + 1][i + 32 * h] << 16;
-      *reinterpret_cast<uint4*>(out + (size_t)c * R + r) = make_uint4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<u32x4*>(out + (size_t)c * R + r) = u32x4{v[0], v[1], v[2], v[3]};
     }
   }
 }
 
-constexpr int kUnsorted = 64;  // up to this many rows are not sorted
-
-int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
-
-// Tiles of M rows that T rows in at most L groups can have.
-int max_tiles(int T, int L, int M) { return T / M + (L < T ? L : T); }
-
-// How a call is cut: a function of its sizes.
+// How a call is cut, and its workspace in order: a function of its sizes.
 struct Plan {
-  bool sorted;
-  int shrink_rows, tiles, slices;  // rows per tile of the shrink, workgroups, pieces of its sum
-  // backward
-  int chunk, pieces, slots;        // rows per piece of the outer products, pieces, partial results of cut groups
+  bool few;
+  int shrink_rows, n_shrink, n_expand, split;
+  int chunk, n_pieces, slots;  // backward: rows per piece of the outer products, pieces, partial results of cut groups
+  size_t offsets, list, shrink, expand, pieces, piece_slots, slot0, part, packed, at, bt, outer_u, outer_v, partial, bytes;
 };
 
-Plan plan_shrink(int T, int K, int L, bool sorted) {
+Plan make_plan(int T, int K, int N, int rank, int L, bool backward) {
   Plan p = {};
-  p.sorted = sorted;
-  p.shrink_rows = T <= 16 && !sorted ? 16 : (T <= 32 || sorted ? 32 : 64);
-  p.tiles = sorted ? max_tiles(T, L, p.shrink_rows) : T;
-  // a piece of 64 k for each of the eight wavefronts at least; about two workgroups a compute unit
-  const int most = ceil_div(K, 64 * kShrinkWaves), want = ceil_div(512, p.tiles > 0 ? p.tiles : 1);
-  p.slices = most < want ? most : want;
-  if (p.slices > 16) p.slices = 16;
-  if (p.slices < 1) p.slices = 1;
-  return p;
-}
-
-Plan plan_backward(int T, int K, int N, int rank, int L) {
-  Plan p = plan_shrink(T, N, L, true);
-  // about 512 workgroups if the rows were one group's; pieces of 256 rows at least
-  const int64_t per_row = (int64_t)(ceil_div(K, kOuterCols) + ceil_div(N, kOuterCols)) * ceil_div(rank, 64);
-  int64_t chunk = (T * per_row / 256 + 255) / 256 * 256;
-  p.chunk = (int)(chunk < 256 ? 256 : (chunk > 8192 ? 8192 : chunk));
-  p.pieces = T / p.chunk + L;
-  p.slots = T > p.chunk ? 2 * (T / p.chunk) : 0;
-  return p;
-}
-
-// The workspace, in order.
-struct Space {
-  size_t offsets, list, slot, sort, part, u, at, bt, outer, bytes;
-};
-Space layout(int T, int K, int N, int rank, int L, bool backward, const Plan& p) {
-  Space s = {};
   size_t at = 0;
   const auto take = [&at](size_t bytes) {
     const size_t here = at;
     at += padded(bytes);
     return here;
   };
-  if (p.sorted) {
-    s.offsets = take((L + 1) * sizeof(int32_t));
-    s.list = take((size_t)T * sizeof(int32_t));
-    s.slot = take((size_t)T * sizeof(int32_t));
-    s.sort = take(permute_workspace_bytes(T, 1, L));
+  p.few = !backward && T <= kFewRows;
+  if (p.few) {
+    p.part = take((size_t)few_pieces(K) * T * rank * sizeof(float));
+    p.bytes = at > 0 ? at : 256;
+    return p;
   }
-  s.part = take((size_t)p.slices * T * rank * sizeof(float));
+  // tiles of 32 rows once those of 16 are more than the compute units (M_a is read for each of them); outer products want 32
+  p.shrink_rows = backward || T > 6144 ? 32 : 16;
+  p.split = 3;  // (two parts for bf16 results)
+  p.n_shrink = (max_tiles(T, L, p.shrink_rows) + 7) / 8 * 8;
+  p.n_expand = max_tiles(T, L + 1, kExpandRows);
+  p.offsets = take((L + 2) * sizeof(int32_t));
+  p.list = take((size_t)T * sizeof(int32_t));
+  p.shrink = take(p.n_shrink * sizeof(Tile));
+  p.expand = take(p.n_expand * sizeof(Tile));
+  p.packed = take(packed_bytes(p.n_shrink * (p.shrink_rows / 16), rank, p.split));
   if (backward) {
-    s.u = take((size_t)T * rank * sizeof(float));
-    s.at = take((size_t)L * K * rank * 2);
-    s.bt = take((size_t)L * N * rank * 2);
-    s.outer = take((size_t)p.slots * rank * ((size_t)K + N) * sizeof(float));
+    p.chunk = outer_chunk(T, ceil_div(K, kOuterCols) + ceil_div(N, kOuterCols), rank, 512);
+    p.n_pieces = T / p.chunk + L;
+    p.slots = T > p.chunk ? 2 * (T / p.chunk) : 0;
+    p.pieces = take(p.n_pieces * sizeof(Tile));
+    p.piece_slots = take(p.n_pieces * sizeof(int32_t));
+    p.slot0 = take(L * sizeof(int32_t));
+    p.at = take((size_t)L * K * rank * 2);
+    p.bt = take((size_t)L * N * rank * 2);
+    p.outer_u = take(outer_bytes(p.n_shrink, rank));
+    p.outer_v = take(outer_bytes(p.n_shrink, rank));
+    p.partial = take((size_t)p.slots * rank * ((size_t)K + N) * sizeof(float));
   }
-  s.bytes = at > 0 ? at : 256;
-  return s;
+  p.bytes = at;
+  return p;
 }
 
-Plan plan_forward(int T, int K, int L) { return plan_shrink(T, K, L, T > kUnsorted); }
-
-hipError_t sort_rows(const int32_t* idx, int T, int L, char* ws, const Space& sp, Rows* rows, hipStream_t s) {
-  int32_t* offsets = reinterpret_cast<int32_t*>(ws + sp.offsets);
-  int32_t* list = reinterpret_cast<int32_t*>(ws + sp.list);
-  *rows = Rows{offsets, list, idx, T, L};
-  return launch_permute(nullptr, idx, T, 1, 8, L, 0, nullptr, offsets, list, reinterpret_cast<int32_t*>(ws + sp.slot), ws + sp.sort,
-                        s);
+template <typename T>
+T* at(char* ws, size_t offset) {
+  return reinterpret_cast<T*>(ws + offset);
 }
 
-template <int MT, int U>
-void launch_shrink_rows(const Rows& rows, const Plan& p, const uint16_t* x, int K, const uint16_t* m, int rank, float* part,
-                        hipStream_t s) {
-  const dim3 grid(p.tiles, p.slices), block(kShrinkWaves * 64);
-  if (rank <= 16) hipLaunchKernelGGL((shrink_kernel<MT, 1, U>), grid, block, 0, s, rows, x, K, m, rank, part);
-  else if (rank <= 32) hipLaunchKernelGGL((shrink_kernel<MT, 2, U>), grid, block, 0, s, rows, x, K, m, rank, part);
-  else if (rank <= 64) hipLaunchKernelGGL((shrink_kernel<MT, 4, 1>), grid, block, 0, s, rows, x, K, m, rank, part);
-  else hipLaunchKernelGGL((shrink_kernel<MT, 8, 1>), grid, block, 0, s, rows, x, K, m, rank, part);
-}
-
-void launch_shrink(Rows rows, const Plan& p, const uint16_t* x, int K, const uint16_t* m, int rank, float* part, hipStream_t s) {
-  if (p.sorted) rows.idx = nullptr;
-  if (p.shrink_rows == 16) launch_shrink_rows<1, 2>(rows, p, x, K, m, rank, part, s);
-  else if (p.shrink_rows == 32) launch_shrink_rows<2, 2>(rows, p, x, K, m, rank, part, s);
-  else launch_shrink_rows<4, 1>(rows, p, x, K, m, rank, part, s);
-}
-
-template <typename YT, int SPLIT, int WCH>
-void launch_expand_width(Expand e, hipStream_t s) {
-  constexpr int M = SPLIT * 32 * WCH <= 256 ? 128 : 64;  // as in the kernel
-  const int T = e.rows.T;
-  const bool sorted = e.rows.offsets != nullptr;
-  e.n_tiles = sorted ? max_tiles(T, e.rows.L, M) : T;
-  const bool bare = sorted && (e.keep != nullptr || (e.y_out != nullptr && e.y_out != e.y_in));
-  const dim3 grid(e.y_out != nullptr ? ceil_div(e.N, kExpandWaves * 64) : 1, e.n_tiles + (bare ? ceil_div(T, 64) : 0));
-  hipLaunchKernelGGL((expand_kernel<YT, SPLIT, WCH, 4, false>), grid, dim3(kExpandThreads), 0, s, e);
-}
-
-template <typename YT, int SPLIT>
-void launch_expand(const Expand& e, hipStream_t s) {
-  if (e.r <= 32) launch_expand_width<YT, SPLIT, 1>(e, s);
-  else if (e.r <= 64) launch_expand_width<YT, SPLIT, 2>(e, s);
-  else launch_expand_width<YT, SPLIT, 4>(e, s);
+void launch_sort(const Plan& p, const int32_t* idx, int T, int L, char* ws, hipStream_t s) {
+  const Sort sort{idx, T, L, p.shrink_rows, p.chunk, p.n_shrink, p.n_expand, p.n_pieces, at<int32_t>(ws, p.offsets),
+                  at<int32_t>(ws, p.list), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0), at<Tile>(ws, p.shrink),
+                  at<Tile>(ws, p.expand), at<Tile>(ws, p.pieces)};
+  hipLaunchKernelGGL(sort_kernel, dim3(1), dim3(kSortThreads), 0, s, sort);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -181,9 +342,7 @@ extern "C" {
 
 size_t moe_lora_workspace_bytes(int32_t T, int32_t K, int32_t N, int32_t rank, int32_t n_adapters, int32_t backward) {
   if (moe::size_status(T, K, N, rank, n_adapters) != MOE_OK) return 0;
-  using namespace moe;
-  const Plan p = backward ? plan_backward(T, K, N, rank, n_adapters) : plan_forward(T, K, n_adapters);
-  return layout(T, K, N, rank, n_adapters, backward != 0, p).bytes;
+  return moe::make_plan(T, K, N, rank, n_adapters, backward != 0).bytes;
 }
 
 int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, int32_t K, int32_t N, int32_t rank,
@@ -201,16 +360,28 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
     return MOE_ERR_WORKSPACE;
   if (T == 0) return MOE_OK;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const Plan p = plan_forward(T, K, n_adapters);
-  const Space sp = layout(T, K, N, rank, n_adapters, false, p);
+  const Plan p = make_plan(T, K, N, rank, n_adapters, false);
   char* const ws = static_cast<char*>(workspace);
-  Rows rows{nullptr, nullptr, adapter_idx, T, n_adapters};
-  if (p.sorted && sort_rows(adapter_idx, T, n_adapters, ws, sp, &rows, s) != hipSuccess) return MOE_ERR_HIP;
-  float* const part = reinterpret_cast<float*>(ws + sp.part);
-  launch_shrink(rows, p, static_cast<const uint16_t*>(x_bf16), K, static_cast<const uint16_t*>(lora_a), rank, part, s);
-  const Expand e{rows, part, p.slices, rank, scale, v, false, static_cast<const uint16_t*>(lora_b), rank, N, y_in, y_out, 0, true};
-  if (flags & MOE_OUT_F32) launch_expand<float, 3>(e, s);
-  else launch_expand<uint16_t, 2>(e, s);
+  const uint16_t *x = static_cast<const uint16_t*>(x_bf16), *a = static_cast<const uint16_t*>(lora_a);
+  const uint16_t* b = static_cast<const uint16_t*>(lora_b);
+  const bool f32 = (flags & MOE_OUT_F32) != 0;
+  if (p.few) {
+    const Few few{adapter_idx, T, n_adapters};
+    float* const part = at<float>(ws, p.part);
+    launch_shrink_few(few, x, K, a, rank, part, s);
+    const ExpandFew e{few, part, few_pieces(K), rank, scale, v, b, N, y_in, y_out};
+    if (f32) launch_expand_few<float, 3>(e, s);
+    else launch_expand_few<uint16_t, 2>(e, s);
+  } else {
+    launch_sort(p, adapter_idx, T, n_adapters, ws, s);
+    const int32_t* list = at<int32_t>(ws, p.list);
+    u32x4* const packed = at<u32x4>(ws, p.packed);
+    launch_shrink(Shrink{at<Tile>(ws, p.shrink), list, x, a, K, rank, f32 ? 3 : 2, scale, v, packed, nullptr}, p.n_shrink,
+                  p.shrink_rows, s);
+    const Expand e{at<Tile>(ws, p.expand), list, T, n_adapters, packed, rank, b, rank, N, y_in, y_out, v};
+    if (f32) launch_expand<float, 3>(e, p.n_expand, s);
+    else launch_expand<uint16_t, 2>(e, p.n_expand, s);
+  }
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -232,33 +403,31 @@ int moe_lora_backward(const void* x_bf16, const void* dy_bf16, const int32_t* ad
     return MOE_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const uint16_t *x = static_cast<const uint16_t*>(x_bf16), *dy = static_cast<const uint16_t*>(dy_bf16);
-  const Plan p = plan_backward(T, K, N, rank, n_adapters);
-  const Space sp = layout(T, K, N, rank, n_adapters, true, p);
+  const Plan p = make_plan(T, K, N, rank, n_adapters, true);
   char* const ws = static_cast<char*>(workspace);
-  Rows rows;
-  if (sort_rows(adapter_idx, T, n_adapters, ws, sp, &rows, s) != hipSuccess) return MOE_ERR_HIP;
-  float *const part = reinterpret_cast<float*>(ws + sp.part), *const u = reinterpret_cast<float*>(ws + sp.u);
-  uint16_t *const at = reinterpret_cast<uint16_t*>(ws + sp.at), *const bt = reinterpret_cast<uint16_t*>(ws + sp.bt);
+  launch_sort(p, adapter_idx, T, n_adapters, ws, s);
+  const int32_t *list = at<int32_t>(ws, p.list), *offsets = at<int32_t>(ws, p.offsets);
+  const Tile* tiles = at<Tile>(ws, p.shrink);
+  u32x4 *const outer_u = at<u32x4>(ws, p.outer_u), *const outer_v = at<u32x4>(ws, p.outer_v);
   if (T > 0) {
     const int ra = ceil_div(rank, 64), ca = ceil_div(K, 64), cb = ceil_div(N, 64);
-    const Transpose tr{{static_cast<const uint16_t*>(lora_a), static_cast<const uint16_t*>(lora_b)}, {at, bt}, {rank, N}, {K, rank},
-                       {ca, ra}, ra * ca, rows.offsets};
-    hipLaunchKernelGGL(transpose_kernel, dim3(ra * (ca + cb), n_adapters), dim3(256), 0, s, tr);
-    launch_shrink(rows, p, dy, N, bt, rank, part, s);
-    const Expand e{rows, part, p.slices, rank, scale, u, true, at, rank, K, dx_in, dx, 0, true};
-    launch_expand<uint16_t, 2>(e, s);
+    uint16_t *const a_t = at<uint16_t>(ws, p.at), *const b_t = at<uint16_t>(ws, p.bt);
+    const Prepare prep{{static_cast<const uint16_t*>(lora_a), static_cast<const uint16_t*>(lora_b)}, {a_t, b_t}, {rank, N}, {K, rank},
+                       {ca, ra}, ra * ca, ra * (ca + cb), n_adapters, offsets,
+                       Pack{tiles, list, T, v, rank, nullptr, outer_v}};
+    hipLaunchKernelGGL(prepare_kernel, dim3(prep.tiles * n_adapters + p.n_shrink), dim3(256), 0, s, prep);
+    u32x4* const packed = at<u32x4>(ws, p.packed);
+    launch_shrink(Shrink{tiles, list, dy, b_t, N, rank, 2, scale, nullptr, packed, outer_u}, p.n_shrink, p.shrink_rows, s);
+    if (dx != nullptr)
+      launch_expand<uint16_t, 2>(Expand{at<Tile>(ws, p.expand), list, T, n_adapters, packed, rank, a_t, rank, K, dx_in, dx, nullptr},
+                                 p.n_expand, s);
   }
-  float* const cut = reinterpret_cast<float*>(ws + sp.outer);
-  const Outer o{{rows.offsets, rows.list, nullptr, T, n_adapters},
-                {{x, u, nullptr, grad_a, cut, K, ceil_div(K, kOuterCols), false},
-                 {dy, v, scale, grad_b, cut + (size_t)p.slots * rank * K, N, ceil_div(N, kOuterCols), true}},
+  float* const partial = at<float>(ws, p.partial);
+  const Outer o{at<Tile>(ws, p.pieces), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0), offsets, list, T, n_adapters,
+                {{x, outer_u, nullptr, grad_a, partial, K, ceil_div(K, kOuterCols), false},
+                 {dy, outer_v, scale, grad_b, partial + (size_t)p.slots * rank * K, N, ceil_div(N, kOuterCols), true}},
                 rank, p.chunk};
-  const dim3 block(kOuterWaves * 64);
-  const int tiles = o.side[0].tiles + o.side[1].tiles;
-  if (rank <= 16) hipLaunchKernelGGL(outer_kernel<1>, dim3(tiles, p.pieces, 1), block, 0, s, o);
-  else if (rank <= 32) hipLaunchKernelGGL(outer_kernel<2>, dim3(tiles, p.pieces, 1), block, 0, s, o);
-  else hipLaunchKernelGGL(outer_kernel<4>, dim3(tiles, p.pieces, ceil_div(rank, 64)), block, 0, s, o);
-  if (p.slots > 0) hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div((int64_t)rank * (K > N ? K : N), 4096), n_adapters), dim3(256), 0, s, o);
+  launch_outer(o, p.n_pieces, p.slots > 0, s);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

@@ -13,9 +13,6 @@ using namespace skinny;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 
-int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
-
 // ---- softmax rows ----------------------------------------------------------------------------------------------------------
 // G lanes (8 to 64) share a token and its E experts, expert l + G s in slot s of the group's lane l: with 8 experts a wavefront holds
 // eight tokens, with 60 one, and every load is of neighbouring words.
@@ -266,13 +263,18 @@ struct LaunchRoute {
 };
 
 // ---- gradient of the router's product --------------------------------------------------------------------------------------
-// d_w_router is the outer product of skinny.hpp over all rows, dx its expansion, with W_r in two bf16 parts: rows [h][part][R] of R =
-// 32, 64, 128 or 256 columns, zeros past E.
-int router_width(int E) { return E <= 32 ? 32 : (E <= 64 ? 64 : (E <= 128 ? 128 : 256)); }
+// d_w_router is the outer product of skinny.hpp over all rows, dx its expansion, with W_r in two bf16 parts: rows [h][part][R] of R
+// columns, E rounded up to a multiple of 32 by zeros.
+int router_width(int E) { return ceil_div(E, 32) * 32; }
 
-__global__ __launch_bounds__(kThreads) void split_router_kernel(const float* __restrict__ w, int64_t n, int E, int R,
-                                                                uint16_t* __restrict__ out) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+// In one launch: W_r's parts, 1024 values a workgroup, and d_logits' fragments, 32 rows a workgroup.
+__global__ __launch_bounds__(kThreads) void router_prepare_kernel(const float* __restrict__ w, int64_t n, int E, int R,
+                                                                  uint16_t* __restrict__ out, int split_blocks, Pack pack) {
+  if (blockIdx.x >= (unsigned)split_blocks) return pack_block(pack, blockIdx.x - split_blocks);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int64_t i = (int64_t)blockIdx.x * 4 * kThreads + k * kThreads + threadIdx.x;
+    if (i >= n) break;
     const int64_t h = i / R;
     const int e = (int)(i - h * R);
     const float v = e < E ? w[h * E + e] : 0.f;
@@ -283,28 +285,20 @@ __global__ __launch_bounds__(kThreads) void split_router_kernel(const float* __r
 }
 
 struct RouterPlan {
-  int chunk, pieces, slots;
-  size_t split, outer, bytes;  // offsets in the workspace
+  int chunk, pieces, slots, blocks;
+  size_t split, packed, outer, partial, bytes;  // offsets in the workspace
 };
 RouterPlan plan_router(int T, int H, int E) {
   RouterPlan p = {};
-  const int tiles = ceil_div(H, kOuterCols) * ceil_div(E, 64);
-  const int chunk = (int)(((int64_t)T * tiles / 256 + 255) / 256 * 256);  // about 256 workgroups, of 256 rows at least
-  p.chunk = chunk < 256 ? 256 : chunk;
+  p.chunk = outer_chunk(T, ceil_div(H, kOuterCols), E, 256);
   p.pieces = T > p.chunk ? ceil_div(T, p.chunk) : 1;
   p.slots = T > p.chunk ? p.pieces : 0;
-  p.split = 0;
-  p.outer = padded((size_t)H * 2 * router_width(E) * 2);
-  p.bytes = p.outer + padded((size_t)p.slots * H * E * sizeof(float));
+  p.blocks = ceil_div(T, 32);
+  p.packed = padded((size_t)H * 2 * router_width(E) * 2);
+  p.outer = p.packed + padded(packed_bytes(2 * p.blocks, E, 2));
+  p.partial = p.outer + padded(outer_bytes(p.blocks, E));
+  p.bytes = p.partial + padded((size_t)p.slots * H * E * sizeof(float));
   return p;
-}
-
-template <int WCH, int NJ>
-void launch_router_expand(Expand e, hipStream_t s) {
-  constexpr int M = 2 * 32 * WCH <= 256 ? 128 : 64;  // as in the kernel
-  e.n_tiles = ceil_div(e.rows.T, M);
-  hipLaunchKernelGGL((expand_kernel<uint16_t, 2, WCH, NJ, true>), dim3(ceil_div(e.N, kExpandWaves * 16 * NJ), e.n_tiles),
-                     dim3(kExpandThreads), 0, s, e);
 }
 
 // ---- gradient of the combine's gates ---------------------------------------------------------------------------------------
@@ -462,27 +456,28 @@ int moe_router_backward(const void* x_bf16, const float* w_router, const float* 
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const RouterPlan p = plan_router(T, H, E);
   char* const ws = static_cast<char*>(workspace);
-  const Rows rows{nullptr, nullptr, nullptr, T, 1};
-  const Outer o{rows,
-                {{static_cast<const uint16_t*>(x_bf16), d_logits, nullptr, d_w_router, reinterpret_cast<float*>(ws + p.outer), H,
+  const int R = router_width(E);
+  uint16_t* const split = reinterpret_cast<uint16_t*>(ws + p.split);
+  u32x4 *const packed = reinterpret_cast<u32x4*>(ws + p.packed), *const outer = reinterpret_cast<u32x4*>(ws + p.outer);
+  if (T > 0) {
+    const int split_blocks = dx != nullptr ? ceil_div((int64_t)H * R, 4 * kThreads) : 0;
+    hipLaunchKernelGGL(router_prepare_kernel, dim3(split_blocks + p.blocks), dim3(kThreads), 0, s, w_router, (int64_t)H * R, E, R, split,
+                       split_blocks, Pack{nullptr, nullptr, T, d_logits, E, dx != nullptr ? packed : nullptr, outer});
+  }
+  const Outer o{nullptr, nullptr, nullptr, nullptr, nullptr, T, 1,
+                {{static_cast<const uint16_t*>(x_bf16), outer, nullptr, d_w_router, reinterpret_cast<float*>(ws + p.partial), H,
                   ceil_div(H, kOuterCols), true},
                  {}},
                 E, p.chunk};
-  const dim3 block(kOuterWaves * 64);
-  if (E <= 16) hipLaunchKernelGGL(outer_kernel<1>, dim3(o.side[0].tiles, p.pieces, 1), block, 0, s, o);
-  else if (E <= 32) hipLaunchKernelGGL(outer_kernel<2>, dim3(o.side[0].tiles, p.pieces, 1), block, 0, s, o);
-  else hipLaunchKernelGGL(outer_kernel<4>, dim3(o.side[0].tiles, p.pieces, ceil_div(E, 64)), block, 0, s, o);
-  if (p.slots > 0) hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div((int64_t)E * H, 4096), 1), dim3(256), 0, s, o);
+  launch_outer(o, p.pieces, p.slots > 0, s);
   if (dx != nullptr && T > 0) {
-    const int R = router_width(E);
-    uint16_t* const split = reinterpret_cast<uint16_t*>(ws + p.split);
-    hipLaunchKernelGGL(split_router_kernel, dim3(ceil_div((int64_t)H * R, 4 * kThreads)), dim3(kThreads), 0, s, w_router,
-                       (int64_t)H * R, E, R, split);
-    const Expand e{rows, d_logits, 1, E, nullptr, nullptr, false, split, 2 * R, H, dx_in, dx, 0, E % 4 == 0 && aligned16(d_logits)};
-    if (R == 32) launch_router_expand<1, 4>(e, s);
-    else if (R == 64) launch_router_expand<2, 4>(e, s);
-    else if (R == 128) launch_router_expand<4, 2>(e, s);
-    else launch_router_expand<8, 2>(e, s);
+    const Expand e{nullptr, nullptr, T, 1, packed, E, split, 2 * R, H, dx_in, dx, nullptr};
+    const int tiles = ceil_div(T, kExpandRows);
+    // M_a's fragments in registers: fewer columns a wavefront for more experts
+    if (R == 32) launch_expand_kernel<uint16_t, 2, 2, 1, 8>(e, tiles, s);
+    else if (R == 64) launch_expand_kernel<uint16_t, 2, 2, 2, 8>(e, tiles, s);
+    else if (R <= 128) launch_expand_kernel<uint16_t, 2, 2, 4, 4>(e, tiles, s);
+    else launch_expand_kernel<uint16_t, 2, 2, 8, 2>(e, tiles, s);
   }
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }

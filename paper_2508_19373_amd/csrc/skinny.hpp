@@ -6,6 +6,11 @@
 // All of them are bound by the one pass over X, Y or Z; the matrix cores do the sums (16x16x32 bf16, fp32 accumulators) with room to
 // spare, so that the narrow fp32 operand P may go in as a sum of bf16 parts: two keep 16 bits of it (enough under a bf16 result's
 // 8), three all 24 (for fp32 results).  The long operand is bf16 as it is, so nothing of it is lost.
+//
+// How the long side is read decides the speed: an MFMA's lanes l, l + 1, ... hold different rows, and a load in that order takes the address
+// unit 64 clocks an instruction (a lane at a time) instead of 16.  So neighbouring lanes read neighbouring 16 bytes of a row, and either
+// LDS (shrink, M_a) or the choice of which columns an accumulator stands for (expand's Y, outer's Z) brings them to the lanes that need
+// them.  P, small and read by every column block, is laid out once in the order of the lanes ("packed").
 #pragma once
 #include "moe_internal.hpp"
 #include "unit_list_wave.hpp"
@@ -13,13 +18,16 @@
 namespace moe {
 namespace skinny {
 
-__device__ __forceinline__ f32x4 mfma(const uint4& a, const uint4& b, f32x4 c) {
+// 16 bytes as the compiler's own vector (arrays of them stay in registers)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(&a), *reinterpret_cast<const bf16x8*>(&b), c, 0,
                                                  0, 0);
 }
 
 // The highest 8 bits of eight floats as bf16; `v` keeps the rest, which is exact.
-__device__ __forceinline__ uint4 take_bf16(float (&v)[8]) {
+__device__ __forceinline__ u32x4 take_bf16(float (&v)[8]) {
   uint32_t p[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -27,173 +35,11 @@ __device__ __forceinline__ uint4 take_bf16(float (&v)[8]) {
     v[2 * i] -= bf16_lo(p[i]);
     v[2 * i + 1] -= bf16_hi(p[i]);
   }
-  return make_uint4(p[0], p[1], p[2], p[3]);
+  return u32x4{p[0], p[1], p[2], p[3]};
 }
-
-// ---- which rows a workgroup works on -----------------------------------------------------------------------------------------
-// A tile: up to M rows of one group.  Rows are given by ids grouped in one of three ways.
-struct Rows {
-  const int32_t* offsets;  // [L+1] first position of each group in `list`; nullptr: not sorted (idx) or all one group (neither)
-  const int32_t* list;     // positions -> rows; nullptr: position = row
-  const int32_t* idx;      // [T] group of each row, for at most 64 rows that nobody has sorted
-  int T, L;
-};
-struct Tile {
-  int group, first, rows;  // group -1: rows without one; rows 0: nothing to do
-};
-
-// The b-th tile of M rows of the sorted groups; with `at_least_one` a group without rows has an empty tile.
-// Four neighbouring groups a lane: their tiles are counted, a scan over the lanes finds the lane, the lane the group.
-__device__ __forceinline__ Tile find_tile(const int32_t* __restrict__ offsets, int L, int M, int b, bool at_least_one) {
-  const int lane = threadIdx.x & (kWave - 1);
-  int o[5], c[4], sum = 0;
-#pragma unroll
-  for (int i = 0; i < 5; ++i) o[i] = offsets[min(4 * lane + i, L)];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    c[i] = (o[i + 1] - o[i] + M - 1) / M;
-    if (at_least_one && 4 * lane + i < L) c[i] = max(c[i], 1);
-    sum += c[i];
-  }
-  const int incl = gg::wave_incl_scan(sum);
-  int rem = b - (incl - sum);
-  const unsigned long long hit = __ballot(rem >= 0 && rem < sum);
-  if (hit == 0) return Tile{-1, 0, 0};
-  int g = 0, first = o[0], end = o[1];
-#pragma unroll
-  for (int i = 0; i < 3; ++i)
-    if (g == i && rem >= c[i]) {
-      rem -= c[i];
-      g = i + 1;
-      first = o[i + 1];
-      end = o[i + 2];
-    }
-  first += rem * M;
-  const int src = __ffsll((long long)hit) - 1;
-  return Tile{(int)__builtin_amdgcn_readlane(4 * lane + g, src), (int)__builtin_amdgcn_readlane(first, src),
-              (int)__builtin_amdgcn_readlane(min(M, end - first), src)};
-}
-
-// Fills s_rows[0 .. rows) and returns the tile.  Every wavefront computes the same; the caller synchronises before it reads s_rows.
-template <int M>
-__device__ __forceinline__ Tile take_tile(const Rows& r, int b, int32_t* s_rows) {
-  const int tid = threadIdx.x, lane = tid & (kWave - 1);
-  if (r.idx != nullptr) {
-    // at most 64 rows (M of them or fewer), a lane each: the first row of a group works for all of them
-    int g = lane < r.T ? r.idx[lane] : -2;
-    if (lane < r.T && (unsigned)g >= (unsigned)r.L) g = -1;
-    const int mine = (int)__builtin_amdgcn_readlane(g, b);
-    const unsigned long long same = __ballot(g == mine);
-    if (__ffsll((long long)same) - 1 != b) return Tile{-1, 0, 0};
-    if (tid < kWave && g == mine) s_rows[__popcll(same & ((1ull << lane) - 1ull))] = lane;
-    return Tile{mine, 0, (int)__popcll(same)};
-  }
-  Tile t{0, b * M, 0};
-  if (r.offsets != nullptr) t = find_tile(r.offsets, r.L, M, b, false);
-  else t.rows = max(0, min(M, r.T - t.first));
-  for (int i = tid; i < t.rows; i += blockDim.x) s_rows[i] = r.list != nullptr ? r.list[t.first + i] : t.first + i;
-  return t;
-}
-
-// ---- shrink ------------------------------------------------------------------------------------------------------------------
-// A wavefront multiplies 16 MT rows by all of M_a over every (8 gridDim.y)-th 64-wide piece of k.  In each piece lane (row, q) loads k =
-// 16 q .. 16 q + 15 of its row, so a row's four lanes read one whole 128-byte line, and so does the lane of M_a: the two MFMAs of a
-// piece take the first and the second half of both, whose sum over k is the same in any order.  The eight wavefronts' results
-// are added in order through LDS; gridDim.y pieces of the sum go to `part` [slice][T][r] (the reader adds them in order).
-// U pieces are in flight before the first product: a prompt batch is a stream of x, a decoding batch a couple of memory round trips.
-constexpr int kShrinkWaves = 8;
-
-template <int MT, int NT, int U>
-__global__ __launch_bounds__(kShrinkWaves * 64) void shrink_kernel(Rows rows, const uint16_t* __restrict__ x, int K,
-                                                                   const uint16_t* __restrict__ m, int r,
-                                                                   float* __restrict__ part) {
-  constexpr int M = 16 * MT;
-  __shared__ int32_t s_rows[M];
-  __shared__ float red[kShrinkWaves][16][NT * 16 + 1];
-  const Tile tile = take_tile<M>(rows, blockIdx.x, s_rows);
-  if (tile.rows == 0 || tile.group < 0) return;
-  __syncthreads();
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = lane & 15, q = lane >> 4;
-  const uint16_t *xr[MT], *mr[NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) xr[i] = x + (size_t)s_rows[min(16 * i + row, tile.rows - 1)] * K + 16 * q;
-#pragma unroll
-  for (int j = 0; j < NT; ++j) mr[j] = m + ((size_t)tile.group * r + min(16 * j + row, r - 1)) * K + 16 * q;
-  f32x4 acc[MT][NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int stride = kShrinkWaves * gridDim.y;
-  for (int c0 = (blockIdx.y * kShrinkWaves + wave) * 64; c0 < K; c0 += stride * 64 * U) {
-    uint4 xv[U][MT][2], mv[U][NT][2];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int k = c0 + u * stride * 64 + 8 * h;
-        const bool in = k + 16 * q < K;  // (K is a multiple of 8)
-#pragma unroll
-        for (int i = 0; i < MT; ++i) xv[u][i][h] = in ? *reinterpret_cast<const uint4*>(xr[i] + k) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) mv[u][j][h] = in ? *reinterpret_cast<const uint4*>(mr[j] + k) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int j = 0; j < NT; ++j) acc[i][j] = mfma(xv[u][i][h], mv[u][j][h], acc[i][j]);
-  }
-  part += (size_t)blockIdx.y * rows.T * r;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    if (16 * i >= tile.rows) break;
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) red[wave][4 * q + e][16 * j + row] = acc[i][j][e];
-    __syncthreads();
-    for (int o = tid; o < 16 * 16 * NT; o += kShrinkWaves * 64) {
-      const int ro = o / (16 * NT), col = o % (16 * NT);
-      float sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < kShrinkWaves; ++w) sum += red[w][ro][col];
-      if (16 * i + ro < tile.rows && col < r) part[(size_t)s_rows[16 * i + ro] * r + col] = sum;
-    }
-    __syncthreads();
-  }
-}
-
-// ---- expand ------------------------------------------------------------------------------------------------------------------
-// A wavefront keeps its 16 NJ rows of M_a (output columns) in registers and walks the tile's rows, 16 at a time.  The MFMA's first operand is
-// M_a, its second P: an accumulator's four values are then four neighbouring columns of one row, and with the columns dealt out
-// as below a lane holds 4 NJ neighbouring ones, so rows of Y are read and written in whole 128-byte lines.  P's parts lie in LDS, a
-// row of them 16 bytes longer than a multiple of 32 so that the lanes' 16-byte reads spread over the banks; narrow sides that are no
-// multiple of 32 end in zeros.  HILO: M_a itself is fp32, given as rows of two bf16 parts; the product of the two low parts (2^-17 of the whole) is
-// left out.
-struct Expand {
-  Rows rows;
-  const float* part;     // [slices][T][r]
-  int slices, r;
-  const float* scale;    // per group, or nullptr
-  float* keep;           // [T][r] the sum over the slices (times scale if keep_scaled), 0 for rows without a group; or nullptr
-  bool keep_scaled;
-  const uint16_t* m;     // [L][N][m_stride]
-  int m_stride, N;
-  const void* y_in;      // [T][N] or nullptr
-  void* y_out;           // nullptr: only `keep`
-  int n_tiles;           // gridDim.y from here on: workgroups for the rows without a group
-  bool vec;              // rows of `part` are made of whole 16-byte pieces
-};
-
-constexpr int kExpandThreads = 256;
-constexpr int kExpandWaves = kExpandThreads / kWave;
 
 __device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
-  const uint4 a = *reinterpret_cast<const uint4*>(p);
+  const u32x4 a = *reinterpret_cast<const u32x4*>(p);
   v[0] = bf16_lo(a.x); v[1] = bf16_hi(a.x); v[2] = bf16_lo(a.y); v[3] = bf16_hi(a.y);
   v[4] = bf16_lo(a.z); v[5] = bf16_hi(a.z); v[6] = bf16_lo(a.w); v[7] = bf16_hi(a.w);
 }
@@ -201,255 +47,662 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
   v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
-__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
-  *reinterpret_cast<uint4*>(p) =
-      make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-}
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+
+inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+inline size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// ---- rows sorted by group ----------------------------------------------------------------------------------------------------
+// Rows in order of their group (of equal groups in their own order), and lists of the work that follows from it: tiles of rows of one
+// group each.  Rows without a group (ids outside [0, L)) come last, as group L.
+struct Tile {
+  int32_t group, first, rows, at;  // first: position in the list; rows 0: nothing to do
+};
+struct Work {
+  const int32_t* offsets;  // [L+2]
+  const int32_t* list;     // positions -> rows
+  const Tile* shrink;      // tiles of shrink_rows; at: their number in the order of the groups
+  const Tile* expand;      // tiles of kExpandRows; at: the number of their first 16 rows
+  const Tile* pieces;      // of up to `chunk` rows, one at least for each group; at: the number of their first 32 rows (shrink_rows == 32)
+  const int32_t* slots;    // the place of a piece's partial result, -1: its group is not cut
+  const int32_t* slot0;    // [L] that of a group's first piece
+};
+constexpr int kExpandRows = 64;
+
+// Tiles of M rows that T rows in at most L groups can have.
+inline int max_tiles(int T, int L, int M) { return T / M + (L < T ? L : T); }
+
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave, kMaxGroups = 256;
+
+struct Sort {
+  const int32_t* idx;
+  int T, L, shrink_rows, chunk;         // chunk 0: no pieces
+  int n_shrink, n_expand, n_pieces;     // entries of the lists
+  int32_t *offsets, *list, *slots, *slot0;
+  Tile *shrink, *expand, *pieces;
+};
+
+// Rank of this lane among the lanes of its wavefront with the same group, and how many there are: a ballot for each bit of the id.
+__device__ __forceinline__ int match_rank(int g, bool in, int lane, int bits, int& count) {
+  unsigned long long same = __ballot(in);
+  for (int b = 0; b < bits; ++b) {
+    const unsigned long long set = __ballot((g >> b) & 1);
+    same &= ((g >> b) & 1) ? set : ~set;
+  }
+  count = __popcll(same);
+  return __popcll(same & ((1ull << lane) - 1ull));
 }
 
-// The rows s_rows[0 .. n) have no group: the output is the input, `keep` is 0.
-template <typename YT>
-__device__ __forceinline__ void copy_rows(const Expand& e, const int32_t* s_rows, int n, int c0, int cols) {
-  const YT* in = static_cast<const YT*>(e.y_in);
-  YT* out = static_cast<YT*>(e.y_out);
-  cols = min(cols, e.N - c0);
-  if (out != nullptr && in != out)
-    for (int i = threadIdx.x; i < n * (cols / 8); i += kExpandThreads) {
-      const size_t at = (size_t)s_rows[i / (cols / 8)] * e.N + c0 + i % (cols / 8) * 8;
-      float v[8] = {};
-      if (in != nullptr) load8(in + at, v);
-      store8(out + at, v);
+// The last entry of pre[0 .. n] (non-decreasing) that is not above v.
+__device__ __forceinline__ int find_group(const int32_t* pre, int n, int v) {
+  int lo = 0, hi = n;  // pre[lo] <= v < pre[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (pre[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// One workgroup: each wavefront counts the groups of its share of the rows, a scan over the groups places them, the wavefronts go
+// over their rows again.  (4096 rows: four steps of 64 a wavefront, each time.  Several workgroups would need launches between the
+// steps, which cost more until there are some ten thousand rows; beyond, the products take longer by far.)
+static __global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
+  __shared__ int32_t cnt[kSortWaves][kMaxGroups + 1];
+  __shared__ int32_t pre[5][kMaxGroups + 2];  // prefixes over the groups of rows, shrink tiles, expand tiles, pieces, slots
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, groups = s.L + 1, bits = 32 - __clz(s.L);
+  const int share = ((s.T + kSortWaves - 1) / kSortWaves + kWave - 1) / kWave * kWave;
+  const int t0 = min(wave * share, s.T), t1 = min(t0 + share, s.T);
+  for (int g = lane; g < groups; g += kWave) cnt[wave][g] = 0;
+  const auto group_at = [&](int t) {
+    const int g = t < t1 ? s.idx[t] : 0;
+    return (unsigned)g < (unsigned)s.L ? g : s.L;
+  };
+  // 64 rows at a time; prompts lie in runs, so often all of them are one group's
+  const auto rank_of = [&](int g, bool in, int& n) {
+    if (__ballot(in && g == (int)__builtin_amdgcn_readfirstlane(g)) == ~0ull) {
+      n = kWave;
+      return lane;
     }
-  if (e.keep != nullptr && c0 == 0)
-    for (int i = threadIdx.x; i < n * e.r; i += kExpandThreads) e.keep[(size_t)s_rows[i / e.r] * e.r + i % e.r] = 0.f;
+    return match_rank(g, in, lane, bits, n);
+  };
+  constexpr int B = 8;
+  for (int t = t0; t < t1; t += B * kWave) {
+    int g[B];
+#pragma unroll
+    for (int u = 0; u < B; ++u) g[u] = group_at(t + u * kWave + lane);
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      if (t + u * kWave >= t1) break;
+      const bool in = t + u * kWave + lane < t1;
+      int n;
+      const int rank = rank_of(g[u], in, n);
+      if (in && rank == 0) cnt[wave][g[u]] += n;
+    }
+  }
+  __syncthreads();
+  for (int g = tid; g < groups; g += kSortThreads) {  // rows of the group in the wavefronts before each; all of them
+    int run = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = cnt[w][g];
+      cnt[w][g] = run;
+      run += c;
+    }
+    pre[0][g] = run;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    int carry[5] = {};
+    for (int g0 = 0; g0 < groups; g0 += kWave) {
+      const int g = g0 + lane;
+      const bool own = g < s.L;
+      const int c = g < groups ? pre[0][g] : 0;
+      int v[5] = {c, own ? (c + s.shrink_rows - 1) / s.shrink_rows : 0, (c + kExpandRows - 1) / kExpandRows, 0, 0};
+      if (s.chunk > 0 && own) {
+        v[3] = max(1, (c + s.chunk - 1) / s.chunk);
+        v[4] = c > s.chunk ? v[3] : 0;
+      }
+#pragma unroll
+      for (int k = 0; k < 5; ++k) {
+        const int incl = gg::wave_incl_scan(v[k]);
+        if (g < groups) pre[k][g] = carry[k] + incl - v[k];
+        carry[k] += (int)__builtin_amdgcn_readlane(incl, kWave - 1);
+      }
+    }
+    if (lane == 0)
+#pragma unroll
+      for (int k = 0; k < 5; ++k) pre[k][groups] = carry[k];
+  }
+  __syncthreads();
+  for (int g = tid; g <= groups; g += kSortThreads) s.offsets[g] = pre[0][g];
+  for (int t = t0; t < t1; t += B * kWave) {
+    int g[B];
+#pragma unroll
+    for (int u = 0; u < B; ++u) g[u] = group_at(t + u * kWave + lane);
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      if (t + u * kWave >= t1) break;
+      const int row = t + u * kWave + lane;
+      const bool in = row < t1;
+      int n;
+      const int rank = rank_of(g[u], in, n);
+      if (in) s.list[pre[0][g[u]] + cnt[wave][g[u]] + rank] = row;
+      if (in && rank == 0) cnt[wave][g[u]] += n;
+    }
+  }
+  // the lists: neighbours in the order of the groups run on one XCD (workgroups b, b + 8, ...), whose L2 then holds few groups' matrices
+  for (int i = tid; i < s.n_shrink + s.n_expand + s.n_pieces; i += kSortThreads) {
+    int b = i, kind = 1;
+    if (i >= s.n_shrink + s.n_expand) b = i - s.n_shrink - s.n_expand, kind = 3;
+    else if (i >= s.n_shrink) b = i - s.n_shrink, kind = 2;
+    int at = b, total = pre[kind][groups];
+    if (kind == 1) {
+      const int per = (total + 7) / 8;
+      b = b / 8 < per ? b % 8 * per + b / 8 : total;
+    }
+    Tile t{kind == 3 ? -1 : 0, 0, 0, 0};
+    int slot = -1;
+    if (b < total) {
+      const int g = find_group(pre[kind], groups, b), p = b - pre[kind][g], n = pre[0][g + 1] - pre[0][g];
+      const int rows = kind == 1 ? s.shrink_rows : (kind == 2 ? kExpandRows : s.chunk), k = p * rows;
+      t = Tile{g, pre[0][g] + k, min(rows, n - k), kind == 1 ? b : (pre[1][g] * s.shrink_rows + k) / (kind == 2 ? 16 : 32)};
+      if (kind == 3) {
+        if (n > s.chunk) slot = pre[4][g] + p;
+        if (p == 0) s.slot0[g] = slot;
+      }
+    }
+    (kind == 1 ? s.shrink : (kind == 2 ? s.expand : s.pieces))[at] = t;
+    if (kind == 3) s.slots[at] = slot;
+  }
 }
 
-template <typename YT, int SPLIT, int WCH, int NJ, bool HILO>
-__global__ __launch_bounds__(kExpandThreads) void expand_kernel(Expand e) {
-  constexpr int R = 32 * WCH, M = SPLIT * R <= 256 ? 128 : 64, COLS = kExpandWaves * 16 * NJ;
-  constexpr int kRowBytes = SPLIT * R * 2 + 16, PARTS = HILO ? 2 : 1, kGroups = NJ / 2;
+// ---- shrink ------------------------------------------------------------------------------------------------------------------
+// A workgroup of 8 wavefronts computes the sums of 16 MT rows, so that they need not be joined by another kernel; a wavefront takes its
+// 8th of k in pieces of 64: 128 bytes of each row, read by eight neighbouring lanes, put into the wavefront's own piece of LDS with the
+// 16-byte parts of a row rearranged by the row's number, and read back as fragments without bank conflicts.  The next U pieces of x are on
+// their way from HBM meanwhile, and the next 32 rows of M_a from L2.  The wavefronts' sums are added in order through LDS.  Tiles begin
+// their walk apart, so that the rows' pieces that the chip reads at one time, a power of two apart in memory, are not those of a
+// few memory channels.
+constexpr int kShrinkWaves = 8, kShrinkThreads = kShrinkWaves * 64;
+
+struct Shrink {
+  const Tile* tiles;
+  const int32_t* list;
+  const uint16_t* x;  // [T][K]
+  const uint16_t* m;  // [L][r][K]
+  int K, r, split;
+  const float* scale;  // per group, for `packed` and `outer`
+  float* keep;         // [T][r] the sums as they are, or nullptr
+  u32x4* packed;       // for expand: [tiles of 16 rows][chunks of 32 columns][split][64]
+  u32x4* outer;        // for outer: [tiles of 32 rows][tiles of 16 columns][3][64], or nullptr (MT == 2 only)
+};
+
+template <int MT, int NT>
+__global__ __launch_bounds__(kShrinkThreads, MT * NT > 8 ? 2 : 4) void shrink_kernel(Shrink a) {
+  constexpr int M = 16 * MT, NG = NT < 2 ? NT : 2, GROUPS = NT / NG, U = MT * NT >= 8 ? 1 : (MT * NT <= 2 ? 4 : 2);
+  constexpr int kWaveBytes = (M + 16 * NG) * 128, kRedStride = NT * 16 + 1, kCols = NT < 2 ? 32 : NT * 16, kSumStride = kCols + 4;
+  constexpr int kRedBytes = kShrinkWaves * 16 * kRedStride * 4, kSumBytes = M * kSumStride * 4, kBytes = kShrinkWaves * kWaveBytes;
   __shared__ int32_t s_rows[M];
-  __shared__ __align__(16) char s_p[M * kRowBytes];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, q = lane >> 4;
-  const int T = e.rows.T, r = e.r;
-  if (blockIdx.y >= (unsigned)e.n_tiles) {  // sorted rows: those that are in no group
-    const int t = (blockIdx.y - e.n_tiles) * 64 + lane;
-    const bool bare = t < T && (unsigned)e.rows.idx[t] >= (unsigned)e.rows.L;
-    const unsigned long long all = __ballot(bare);
-    if (all == 0) return;
-    if (bare && wave == 0) s_rows[__popcll(all & ((1ull << lane) - 1ull))] = t;
-    __syncthreads();
-    copy_rows<YT>(e, s_rows, __popcll(all), blockIdx.x * COLS, COLS);
-    return;
-  }
-  Rows sorted = e.rows;
-  if (sorted.offsets != nullptr) sorted.idx = nullptr;
-  const Tile tile = take_tile<M>(sorted, blockIdx.y, s_rows);
+  __shared__ __align__(16) char s_buf[kBytes > kRedBytes + kSumBytes ? kBytes : kRedBytes + kSumBytes];
+  const Tile tile = a.tiles[blockIdx.x];
   if (tile.rows == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, q = lane >> 4, sub = lane >> 3, ch = lane & 7;
+  const int K = a.K, r = a.r;
+  if (tid < M) s_rows[tid] = a.list[tile.first + min(tid, tile.rows - 1)];
+  const uint16_t* xr[2 * MT];
+#pragma unroll
+  for (int i = 0; i < 2 * MT; ++i) xr[i] = a.x + (size_t)a.list[tile.first + min(8 * i + sub, tile.rows - 1)] * K + 8 * ch;
+  const uint16_t* const mg = a.m + (size_t)tile.group * r * K + 8 * ch;
+  char* const s_x = s_buf + wave * kWaveBytes;
+  char* const s_m = s_x + M * 128;
+  const int put = sub * 128 + (ch ^ sub) * 16;  // + 1024 for each eight rows
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int pieces = (K + 63) / 64, first = pieces * wave / kShrinkWaves, n = pieces * (wave + 1) / kShrinkWaves - first;
+  // Straight-line code: a load under a condition makes the compiler wait for all loads.  Past the end the last piece is loaded again,
+  // past K the first columns, and x's part set to zero.
+  u32x4 xv[U][2 * MT], mv[2 * NG];
+  const int turn = n > 0 ? tile.at % n : 0;
+  const auto piece = [&](int i) {
+    i = min(i, n - 1) + turn;
+    return (first + (i < n ? i : i - n)) * 64;
+  };
+  const auto load_x = [&](u32x4(&v)[2 * MT], int c) {
+    c = c + 8 * ch < K ? c : -8 * ch;  // (K is a multiple of 8)
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) v[i] = *reinterpret_cast<const u32x4*>(xr[i] + c);
+  };
+  const auto load_m = [&](int c, int g) {
+    c = c + 8 * ch < K ? c : -8 * ch;
+#pragma unroll
+    for (int i = 0; i < 2 * NG; ++i) mv[i] = *reinterpret_cast<const u32x4*>(mg + (size_t)min(32 * g + 8 * i + sub, r - 1) * K + c);
+  };
+  if (n > 0) {
+    load_m(piece(0), 0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_x(xv[u], piece(u));
+    for (int i0 = 0; i0 < n; i0 += U) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u;
+        const bool in = i < n && piece(i) + 8 * ch < K;
+#pragma unroll
+        for (int k = 0; k < 2 * MT; ++k) {
+          const u32x4 v = xv[u][k];
+          *reinterpret_cast<u32x4*>(s_x + put + 1024 * k) = u32x4{in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u};
+        }
+        u32x4 f[MT][2];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            f[t][h] = *reinterpret_cast<const u32x4*>(s_x + (16 * t + ln) * 128 + (((4 * h + q) ^ (ln & 7)) * 16));
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+#pragma unroll
+          for (int k = 0; k < 2 * NG; ++k) *reinterpret_cast<u32x4*>(s_m + put + 1024 * k) = mv[k];
+          if (g + 1 < GROUPS) load_m(piece(i), g + 1);
+          else {  // M_a's first: loads return in order, and it is waited for first
+            load_m(piece(i + 1), 0);
+            __builtin_amdgcn_sched_barrier(0);
+            load_x(xv[u], piece(i + U));
+          }
+#pragma unroll
+          for (int j = 0; j < NG; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const u32x4 b = *reinterpret_cast<const u32x4*>(s_m + (16 * j + ln) * 128 + (((4 * h + q) ^ (ln & 7)) * 16));
+#pragma unroll
+              for (int t = 0; t < MT; ++t) acc[t][g * NG + j] = mfma(f[t][h], b, acc[t][g * NG + j]);
+            }
+        }
+      }
+    }
+  }
+  float* const red = reinterpret_cast<float*>(s_buf);              // [wave][16][kRedStride]
+  float* const sum = reinterpret_cast<float*>(s_buf + kRedBytes);  // [M][kSumStride], zeros past the rows and past r
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) red[(wave * 16 + 4 * q + e) * kRedStride + 16 * j + ln] = acc[t][j][e];
+    __syncthreads();
+    for (int o = tid; o < 16 * kCols; o += kShrinkThreads) {
+      const int ro = o / kCols, col = o % kCols;
+      float v = 0.f;
+      if (16 * t + ro < tile.rows && col < r) {
+#pragma unroll
+        for (int w = 0; w < kShrinkWaves; ++w) v += red[(w * 16 + ro) * kRedStride + col];
+        if (a.keep != nullptr) a.keep[(size_t)s_rows[16 * t + ro] * r + col] = v;
+      }
+      sum[(16 * t + ro) * kSumStride + col] = v;
+    }
+  }
   __syncthreads();
-  if (tile.group < 0) {
-    copy_rows<YT>(e, s_rows, tile.rows, blockIdx.x * COLS, COLS);
+  const float scale = a.scale[tile.group];
+  const int chunks = (r + 31) / 32;
+  for (int o = tid; o < MT * chunks * 64; o += kShrinkThreads) {  // lane (row, 8 columns)
+    const int l = o & 63, c = (o >> 6) % chunks, t = (o >> 6) / chunks;
+    float v[8];
+    load8(sum + (16 * t + (l & 15)) * kSumStride + 32 * c + 8 * (l >> 4), v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= scale;
+    u32x4* const to = a.packed + (((size_t)tile.at * MT + t) * chunks + c) * a.split * 64 + l;
+    for (int s = 0; s < a.split; ++s) to[s * 64] = take_bf16(v);
+  }
+  if (MT == 2 && a.outer != nullptr) {
+    const int tiles = (r + 15) / 16;
+    for (int o = tid; o < tiles * 64; o += kShrinkThreads) {  // lane (column, 8 rows)
+      const int l = o & 63, m = o >> 6;
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = scale * sum[(8 * (l >> 4) + k) * kSumStride + 16 * m + (l & 15)];
+      u32x4* const to = a.outer + ((size_t)tile.at * tiles + m) * 3 * 64 + l;
+#pragma unroll
+      for (int s = 0; s < 3; ++s) to[s * 64] = take_bf16(v);
+    }
+  }
+}
+
+inline void launch_shrink(const Shrink& a, int n_tiles, int rows, hipStream_t s) {
+  const dim3 grid(n_tiles), block(kShrinkThreads);
+  if (rows == 16) {
+    if (a.r <= 16) hipLaunchKernelGGL((shrink_kernel<1, 1>), grid, block, 0, s, a);
+    else if (a.r <= 32) hipLaunchKernelGGL((shrink_kernel<1, 2>), grid, block, 0, s, a);
+    else if (a.r <= 64) hipLaunchKernelGGL((shrink_kernel<1, 4>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((shrink_kernel<1, 8>), grid, block, 0, s, a);
+  } else {
+    if (a.r <= 16) hipLaunchKernelGGL((shrink_kernel<2, 1>), grid, block, 0, s, a);
+    else if (a.r <= 32) hipLaunchKernelGGL((shrink_kernel<2, 2>), grid, block, 0, s, a);
+    else if (a.r <= 64) hipLaunchKernelGGL((shrink_kernel<2, 4>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((shrink_kernel<2, 8>), grid, block, 0, s, a);
+  }
+}
+
+// ---- packing a P that is there already ----------------------------------------------------------------------------------------
+struct Pack {
+  const Tile* tiles;    // of 32 rows; nullptr: all rows one group
+  const int32_t* list;
+  int T;
+  const float* p;       // [T][r]
+  int r;
+  u32x4* packed;        // as Shrink's, in two parts; or nullptr
+  u32x4* outer;
+};
+__device__ __forceinline__ void pack_block(const Pack& a, int b) {
+  Tile t{0, b * 32, 0, b};
+  if (a.tiles != nullptr) t = a.tiles[b];
+  else t.rows = min(32, a.T - t.first);
+  if (t.rows == 0) return;
+  const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4, r = a.r, tiles = (r + 15) / 16, chunks = (r + 31) / 32;
+  const auto value = [&](int i, int j) {
+    if (i >= t.rows || j >= r) return 0.f;
+    const int at = t.first + i;
+    return a.p[(size_t)(a.list != nullptr ? a.list[at] : at) * r + j];
+  };
+  const int waves = blockDim.x >> 6;
+  for (int m = threadIdx.x >> 6; m < tiles; m += waves) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = value(8 * q + i, 16 * m + c);
+    u32x4* const to = a.outer + ((size_t)t.at * tiles + m) * 3 * 64 + lane;
+#pragma unroll
+    for (int s = 0; s < 3; ++s) to[s * 64] = take_bf16(v);
+  }
+  if (a.packed == nullptr) return;
+  for (int o = threadIdx.x >> 6; o < 2 * chunks; o += waves) {
+    const int h = o & 1, k = o >> 1;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = value(16 * h + c, 32 * k + 8 * q + i);
+    u32x4* const to = a.packed + (((size_t)t.at * 2 + h) * chunks + k) * 2 * 64 + lane;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) to[s * 64] = take_bf16(v);
+  }
+}
+
+// Bytes of both forms for n tiles of 16 and of 32 rows.
+inline size_t packed_bytes(int n, int r, int split) { return (size_t)n * ceil_div(r, 32) * split * 1024; }
+inline size_t outer_bytes(int n, int r) { return (size_t)n * ceil_div(r, 16) * 3 * 1024; }
+
+// ---- expand ------------------------------------------------------------------------------------------------------------------
+// A wavefront computes up to 64 rows of 16 NJ columns, 16 rows at a time.  The MFMA's first operand is P, its second M_a; accumulator j of
+// lane c stands for column NJ c + j (of fp32 results 4 c + j % 4 of every 64), so that a lane's values of one row are neighbours and the 16
+// lanes of a row read and write up to 256 bytes in a row.  M_a's fragments stay in registers; they come through the wavefront's own LDS,
+// where they are put as they lie in memory.  The next 16 rows' P and Y are on their way during a step's products.  PARTS == 2: M_a itself is
+// fp32, given as rows of two bf16 parts; the product of the two low parts (2^-17 of the whole) is left out.
+constexpr int kExpandThreads = 256, kExpandWaves = kExpandThreads / kWave;
+
+struct Expand {
+  const Tile* tiles;    // nullptr: all rows one group
+  const int32_t* list;
+  int T, L;
+  const u32x4* packed;
+  int r;
+  const uint16_t* m;    // [L][N][m_stride]
+  int m_stride, N;
+  const void* y_in;     // [T][N] or nullptr
+  void* y_out;          // [T][N]
+  float* keep;          // zeroed for rows without a group, or nullptr
+};
+
+// `n` rows without a group: the output is the input, `keep` is 0.
+template <typename YT>
+__device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, float* keep, int r, int N, const int32_t* s_rows, int n, int c0,
+                                          int cols) {
+  constexpr int W = 16 / sizeof(YT);
+  const YT* in = static_cast<const YT*>(y_in);
+  YT* out = static_cast<YT*>(y_out);
+  cols = min(cols, N - c0);
+  if (in != out) {
+    const int per_row = cols / W, total = n * per_row;
+    for (int i0 = threadIdx.x; i0 < total; i0 += 8 * kExpandThreads) {
+      u32x4 v[8];
+      size_t at[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = min(i0 + u * kExpandThreads, total - 1);
+        at[u] = (size_t)s_rows[i / per_row] * N + c0 + i % per_row * W;
+        v[u] = in != nullptr ? *reinterpret_cast<const u32x4*>(in + at[u]) : u32x4{};
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u * kExpandThreads < total) *reinterpret_cast<u32x4*>(out + at[u]) = v[u];
+    }
+  }
+  if (keep != nullptr && c0 == 0)
+    for (int i = threadIdx.x; i < n * r; i += kExpandThreads) keep[(size_t)s_rows[i / r] * r + i % r] = 0.f;
+}
+
+template <typename YT, int SPLIT, int PARTS, int CH, int NJ>
+__global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e) {
+  constexpr int BYTES = NJ * (int)sizeof(YT) < 16 ? NJ * (int)sizeof(YT) : 16, W = BYTES / (int)sizeof(YT), UNITS = NJ / W;
+  constexpr int COLS = 16 * NJ, U = kExpandRows / 16;
+  typedef uint32_t unit __attribute__((ext_vector_type(BYTES / 4)));
+  __shared__ int32_t s_rows[kExpandRows];
+  __shared__ __align__(16) char s_buf[kExpandWaves * COLS * 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, q = lane >> 4;
+  Tile tile{0, (int)blockIdx.y * kExpandRows, 0, (int)blockIdx.y * U};
+  if (e.tiles != nullptr) tile = e.tiles[blockIdx.y];
+  else tile.rows = min(kExpandRows, e.T - tile.first);
+  if (tile.rows == 0) return;
+  if (tid < kExpandRows) {
+    const int at = tile.first + min(tid, tile.rows - 1);
+    s_rows[tid] = e.list != nullptr ? e.list[at] : at;
+  }
+  __syncthreads();
+  if (tile.group == e.L) {
+    copy_rows<YT>(e.y_in, e.y_out, e.keep, e.r, e.N, s_rows, tile.rows, blockIdx.x * kExpandWaves * COLS, kExpandWaves * COLS);
     return;
   }
-  const int nbase = (blockIdx.x * kExpandWaves + wave) * 16 * NJ;
-  uint4 w[PARTS][WCH][NJ];
-  if (e.y_out != nullptr) {
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int n = nbase + (ln >> 2) * (4 * NJ) + 4 * j + (ln & 3);
-      const uint16_t* mr = e.m + ((size_t)tile.group * e.N + min(n, e.N - 1)) * e.m_stride + 8 * q;
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-        for (int c = 0; c < WCH; ++c)
-          w[p][c][j] = (HILO || 32 * c + 8 * q < r) ? *reinterpret_cast<const uint4*>(mr + p * R + 32 * c) : make_uint4(0, 0, 0, 0);
-    }
-  }
-  const float scale = e.scale != nullptr ? e.scale[tile.group] : 1.f;
-  const int row_tiles = (tile.rows + 15) / 16;
-  const size_t slice = (size_t)T * r;
-  for (int o = tid; o < row_tiles * 16 * (R / 8); o += kExpandThreads) {
-    const int i = o / (R / 8), j0 = o % (R / 8) * 8;
-    float v[8] = {};
-    if (i < tile.rows && j0 < r) {
-      const size_t at = (size_t)s_rows[i] * r + j0;
-      if (e.vec) {
-        const bool second = j0 + 4 < r;
-        for (int s = 0; s < e.slices; ++s) {
-          const float4 a = *reinterpret_cast<const float4*>(e.part + s * slice + at);
-          const float4 b = second ? *reinterpret_cast<const float4*>(e.part + s * slice + at + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-          v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
-        }
-      } else {
-        for (int s = 0; s < e.slices; ++s)
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (j0 + k < r) v[k] += e.part[s * slice + at + k];
-      }
-      if (e.keep != nullptr && blockIdx.x == 0)
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (j0 + k < r) e.keep[at + k] = e.keep_scaled ? scale * v[k] : v[k];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] *= scale;
-    }
-#pragma unroll
-    for (int p = 0; p < SPLIT; ++p) *reinterpret_cast<uint4*>(s_p + i * kRowBytes + p * R * 2 + j0 * 2) = take_bf16(v);
-  }
-  __syncthreads();
-  if (e.y_out == nullptr || nbase >= e.N) return;
+  const int nbase = (blockIdx.x * kExpandWaves + wave) * COLS;
+  if (nbase >= e.N) return;
+  const int chunks = (e.r + 31) / 32;
   const YT* in = static_cast<const YT*>(e.y_in);
   YT* out = static_cast<YT*>(e.y_out);
-  const int c0 = nbase + q * (4 * NJ);
-  constexpr int U = 4;
-  for (int tt0 = 0; tt0 < row_tiles; tt0 += U) {
-    float y[U][kGroups][8];
-    size_t at[U];
+  const int c0 = nbase + ln * W;
+  unit y[2][4][UNITS];
+  u32x4 p[2][CH][SPLIT];
+  // (no load under a condition: the compiler would wait for all loads behind it)
+  const unit* const base = in != nullptr ? reinterpret_cast<const unit*>(in) : reinterpret_cast<const unit*>(e.packed);
+  const int in_last = in != nullptr ? e.N - W : 0;
+  const size_t in_stride = in != nullptr ? e.N : 0;
+  const auto load = [&](unit(&yy)[4][UNITS], u32x4(&pp)[CH][SPLIT], int u) {
+    const u32x4* const from = e.packed + ((size_t)tile.at + u) * chunks * SPLIT * 64 + lane;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      at[u] = (size_t)s_rows[min((tt0 + u) * 16 + ln, tile.rows - 1)] * e.N + c0;
+    for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int h = 0; h < kGroups; ++h) {
+      for (int s = 0; s < SPLIT; ++s) pp[c][s] = from[(min(c, chunks - 1) * SPLIT + s) * 64];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[u][h][k] = 0.f;
-        if (in != nullptr && c0 + 8 * h < e.N && (tt0 + u) * 16 + ln < tile.rows) load8(in + at[u] + 8 * h, y[u][h]);
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int h = 0; h < UNITS; ++h)
+        yy[k][h] = *reinterpret_cast<const unit*>(reinterpret_cast<const YT*>(base) + s_rows[16 * u + 4 * q + k] * in_stride +
+                                                  min(c0 + 64 * h, in_last));
+  };
+  // M_a: 32 columns at a time into LDS, a row's four 16-byte parts rearranged so that both sides meet few bank conflicts
+  u32x4 w[PARTS][CH][NJ];
+  char* const s_m = s_buf + wave * COLS * 64;
+  const uint16_t* const mr = e.m + ((size_t)tile.group * e.N + nbase) * e.m_stride;
+  const int m_cols = PARTS == 2 ? 32 * chunks : e.r;
+#pragma unroll
+  for (int pt = 0; pt < PARTS; ++pt)
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < NJ; ++i) {
+        const int n = min(16 * i + (lane >> 2), e.N - 1 - nbase), col = 32 * c + 8 * (lane & 3);
+        w[pt][c][i] = *reinterpret_cast<const u32x4*>(mr + (size_t)n * e.m_stride + (col < m_cols ? pt * 32 * chunks + col : 0));
+      }
+  const int last = (tile.rows - 1) / 16;
+  load(y[0], p[0], 0);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int pt = 0; pt < PARTS; ++pt)
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+#pragma unroll
+      for (int i = 0; i < NJ; ++i) {  // column n: accumulator and lane
+        const int n = 16 * i + (lane >> 2);
+        const int j = sizeof(YT) == 2 ? n % NJ : (n >> 6) * 4 + (n & 3), l = sizeof(YT) == 2 ? n / NJ : (n >> 2) & 15;
+        const bool zero = 32 * c + 8 * (lane & 3) >= m_cols;
+        const u32x4 v = w[pt][c][i];
+        *reinterpret_cast<u32x4*>(s_m + (j * 16 + l) * 64 + (((lane & 3) ^ (l >> 1 & 3)) * 16)) =
+            u32x4{zero ? 0u : v.x, zero ? 0u : v.y, zero ? 0u : v.z, zero ? 0u : v.w};
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        w[pt][c][j] = *reinterpret_cast<const u32x4*>(s_m + (j * 16 + ln) * 64 + ((q ^ (ln >> 1 & 3)) * 16));
+    }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (16 * u >= tile.rows) break;
+    if (u + 1 < U) load(y[(u + 1) & 1], p[(u + 1) & 1], min(u + 1, last));
+    f32x4 acc[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int s = SPLIT - 1; s >= 0; --s) {  // the small parts first
+        const u32x4 a = p[u & 1][c][s];
+        if (PARTS == 2 && s == 0)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[j] = mfma(a, w[PARTS - 1][c][j], acc[j]);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[j] = mfma(a, w[0][c][j], acc[j]);
+      }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (16 * u + 4 * q + k >= tile.rows) continue;
+#pragma unroll
+      for (int h = 0; h < UNITS; ++h) {
+        if (c0 + 64 * h >= e.N) continue;
+        unit o;
+#pragma unroll
+        for (int i = 0; i < BYTES / 4; ++i) {
+          const uint32_t d = in != nullptr ? y[u & 1][k][h][i] : 0u;
+          if constexpr (sizeof(YT) == 2) o[i] = pack_bf16x2(bf16_lo(d) + acc[2 * i][k], bf16_hi(d) + acc[2 * i + 1][k]);
+          else o[i] = __float_as_uint(__uint_as_float(d) + acc[4 * h + i][k]);
+        }
+        *reinterpret_cast<unit*>(out + (size_t)s_rows[16 * u + 4 * q + k] * e.N + c0 + 64 * h) = o;
       }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (tt0 + u >= row_tiles) break;
-      f32x4 acc[NJ];
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const char* p = s_p + ((tt0 + u) * 16 + ln) * kRowBytes + q * 16;
-#pragma unroll
-      for (int c = 0; c < WCH; ++c)
-#pragma unroll
-        for (int s = SPLIT - 1; s >= 0; --s) {  // the small parts first
-          const uint4 b = *reinterpret_cast<const uint4*>(p + s * R * 2 + c * 64);
-#pragma unroll
-          for (int j = 0; j < NJ; ++j) acc[j] = mfma(w[0][c][j], b, acc[j]);
-          if (HILO && s == 0)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[j] = mfma(w[PARTS - 1][c][j], b, acc[j]);
-        }
-      if ((tt0 + u) * 16 + ln < tile.rows)
-#pragma unroll
-        for (int h = 0; h < kGroups; ++h)
-          if (c0 + 8 * h < e.N) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) y[u][h][k] += acc[2 * h + k / 4][k % 4];
-            store8(out + at[u] + 8 * h, y[u][h]);
-          }
-    }
   }
+}
+
+template <typename YT, int SPLIT, int PARTS, int CH, int NJ>
+void launch_expand_kernel(const Expand& e, int n_tiles, hipStream_t s) {
+  hipLaunchKernelGGL((expand_kernel<YT, SPLIT, PARTS, CH, NJ>), dim3(ceil_div(e.N, kExpandWaves * 16 * NJ), n_tiles),
+                     dim3(kExpandThreads), 0, s, e);
 }
 
 // ---- outer -------------------------------------------------------------------------------------------------------------------
 // A wavefront takes 32 rows at a time: lane (c, q) loads 8 neighbouring columns of rows 8 q .. 8 q + 7, a row's 16 lanes 256 bytes in a
 // row, and byte permutations turn the eight 16-byte rows into eight column fragments (rows are the sum's index): no trip through
-// LDS.  P's fragments are read as they lie and split in three parts.  The eight wavefronts take every eighth 32 rows; their sums are
-// added in order through LDS, 16 of P's columns at a time.  A group of more than `chunk` rows is cut, its pieces' sums go to `part`
-// and join in reduce_kernel: which pieces there are follows from the rows alone, so the order of the additions is fixed.
+// LDS.  P's fragments come packed in three parts.  The wavefronts take every fourth 32 rows; their sums are added in order through LDS,
+// one tile of P's columns at a time.  A group of more than `chunk` rows is cut, its pieces' sums go to `part` and join in
+// reduce_kernel: which pieces there are follows from the rows alone, so the order of the additions is fixed.
 struct OuterSide {
-  const uint16_t* z;   // [T][cols]
-  const float* p;      // [T][r]
-  const float* scale;  // per group, or nullptr
-  float* out;          // [L][r][cols], or [L][cols][r] if by_column
-  float* part;         // the same for each piece of a cut group
-  int cols, tiles;     // tiles of 128 columns
+  const uint16_t* z;    // [T][cols]
+  const u32x4* packed;
+  const float* scale;   // per group, or nullptr
+  float* out;           // [L][r][cols], or [L][cols][r] if by_column
+  float* part;          // the same for each piece of a cut group
+  int cols, tiles;      // tiles of 128 columns
   bool by_column;
 };
 struct Outer {
-  Rows rows;
+  const Tile* pieces;   // nullptr: all rows one group
+  const int32_t *slots, *slot0, *offsets, *list;
+  int T, L;
   OuterSide side[2];
-  int r, chunk;
+  int r, chunk;         // rows of a piece, a multiple of 32
 };
 
-constexpr int kOuterWaves = 8, kOuterCols = 128;
-
-// The place of the b-th piece in `part`: the pieces of cut groups before it; -1: its group is not cut.
-__device__ __forceinline__ int piece_slot(const Rows& rows, int chunk, const Tile& t) {
-  const int lane = threadIdx.x & (kWave - 1);
-  if (rows.offsets == nullptr) return rows.T > chunk ? t.first / chunk : -1;
-  int before = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int g = 4 * lane + i;
-    const int n = g < t.group ? rows.offsets[min(g + 1, rows.L)] - rows.offsets[min(g, rows.L)] : 0;
-    if (n > chunk) before += (n + chunk - 1) / chunk;
-  }
-  before = (int)__builtin_amdgcn_readlane(gg::wave_incl_scan(before), kWave - 1);
-  const int first = rows.offsets[t.group], n = rows.offsets[t.group + 1] - first;
-  return n > chunk ? before + (t.first - first) / chunk : -1;
-}
+constexpr int kOuterWaves = 4, kOuterThreads = kOuterWaves * 64, kOuterCols = 128, kMaxChunk = 4096;
 
 template <int MT>
-__global__ __launch_bounds__(kOuterWaves * 64) void outer_kernel(Outer o) {
-  __shared__ float red[kOuterWaves][16][kOuterCols + 4];
-  const OuterSide& sd = o.side[blockIdx.x >= (unsigned)o.side[0].tiles];
-  const int col_tile = blockIdx.x >= (unsigned)o.side[0].tiles ? blockIdx.x - o.side[0].tiles : blockIdx.x;
-  Tile tile{0, (int)blockIdx.y * o.chunk, 0};
-  if (o.rows.offsets != nullptr) tile = find_tile(o.rows.offsets, o.rows.L, o.chunk, blockIdx.y, true);
-  else tile.rows = min(o.chunk, o.rows.T - tile.first);
+__global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
+  __shared__ __align__(16) char s_buf[kOuterWaves * 16 * (kOuterCols + 4) * 4];
+  static_assert(sizeof(s_buf) >= kMaxChunk * 4, "the rows' numbers lie where the sums are joined later");
+  int32_t* const s_rows = reinterpret_cast<int32_t*>(s_buf);
+  float(*const red)[16][kOuterCols + 4] = reinterpret_cast<float(*)[16][kOuterCols + 4]>(s_buf);
+  const bool second = blockIdx.x >= (unsigned)o.side[0].tiles;
+  const OuterSide sd = second ? o.side[1] : o.side[0];
+  const int col_tile = second ? blockIdx.x - o.side[0].tiles : blockIdx.x;
+  Tile tile{0, (int)blockIdx.y * o.chunk, 0, (int)blockIdx.y * (o.chunk / 32)};
+  if (o.pieces != nullptr) tile = o.pieces[blockIdx.y];
+  else tile.rows = min(o.chunk, o.T - tile.first);
   if (tile.group < 0) return;
-  const int slot = piece_slot(o.rows, o.chunk, tile);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, q = lane >> 4;
-  const int r = o.r, r0 = blockIdx.z * 16 * MT, c0 = col_tile * kOuterCols;
+  if (o.list != nullptr) {
+    for (int i = tid; i < tile.rows; i += kOuterThreads) s_rows[i] = o.list[tile.first + i];
+    __syncthreads();
+  }
+  const int r = o.r, tiles = (r + 15) / 16, m0 = blockIdx.z * MT, c0 = col_tile * kOuterCols;
   f32x4 acc[MT][8];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int zc = min(c0 + 8 * c, sd.cols - 8);  // columns past the end are computed and not stored
-  for (int s0 = wave * 32; s0 < tile.rows; s0 += kOuterWaves * 32) {
-    int row[8];
-    uint4 z[8];
-    float p[MT][8];
+  const uint16_t* const zc = sd.z + min(c0 + 8 * c, sd.cols - 8);  // columns past the end are computed and not stored
+  const int blocks = (tile.rows + 31) / 32;
+  const u32x4* const packed = sd.packed + ((size_t)tile.at * tiles + m0) * 3 * 64 + lane;
+  const int m_last = min(MT, tiles - m0) - 1;  // (tiles past the last: computed from it again and not stored)
+  u32x4 z[8];
+  const auto load_z = [&](int b) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int at = min(s0 + 8 * q + i, tile.rows - 1);  // (past the end: a row of the same group, times 0)
-      row[i] = o.rows.list != nullptr ? o.rows.list[tile.first + at] : tile.first + at;
+      const int at = min(32 * b + 8 * q + i, tile.rows - 1);  // (past the end: a row of the same group, times 0)
+      z[i] = *reinterpret_cast<const u32x4*>(zc + (size_t)(o.list != nullptr ? s_rows[at] : tile.first + at) * sd.cols);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = *reinterpret_cast<const uint4*>(sd.z + (size_t)row[i] * sd.cols + zc);
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int j = r0 + 16 * m + c;
-        p[m][i] = (j < r && s0 + 8 * q + i < tile.rows) ? sd.p[(size_t)row[i] * r + j] : 0.f;
-      }
-    uint4 f[8];
+  };
+  int b = wave;
+  if (b < blocks) load_z(b);
+  for (; b < blocks; b += kOuterWaves) {
+    u32x4 f[8];
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
       uint32_t lo[4], hi[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t a = reinterpret_cast<const uint32_t*>(&z[2 * i])[d], b = reinterpret_cast<const uint32_t*>(&z[2 * i + 1])[d];
-        lo[i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
-        hi[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        const uint32_t x = z[2 * i][d], y = z[2 * i + 1][d];
+        lo[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+        hi[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
       }
-      f[2 * d] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-      f[2 * d + 1] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      f[2 * d] = u32x4{lo[0], lo[1], lo[2], lo[3]};
+      f[2 * d + 1] = u32x4{hi[0], hi[1], hi[2], hi[3]};
     }
+    const u32x4* const from = packed + (size_t)b * tiles * 3 * 64;
+    u32x4 p[2][3];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int s = 0; s < 3; ++s) p[0][s] = from[s * 64];
 #pragma unroll
-      for (int s = 0; s < 3; ++s) {
-        const uint4 a = take_bf16(p[m]);
+    for (int m = 0; m < MT; ++m) {
+      if (m + 1 < MT)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[m][j] = mfma(a, f[j], acc[m][j]);
-      }
+        for (int s = 0; s < 3; ++s) p[(m + 1) & 1][s] = from[min(m + 1, m_last) * 3 * 64 + s * 64];
+      else  // Z's next rows behind the last of P: loads return in order
+        load_z(min(b + kOuterWaves, blocks - 1));
+#pragma unroll
+      for (int s = 0; s < 3; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[m][j] = mfma(p[m & 1][s], f[j], acc[m][j]);
+    }
   }
+  const int slot = o.pieces != nullptr ? o.slots[blockIdx.y] : (o.T > o.chunk ? (int)blockIdx.y : -1);
   const float scale = sd.scale != nullptr ? sd.scale[tile.group] : 1.f;
   float* out = slot >= 0 ? sd.part + (size_t)slot * r * sd.cols : sd.out + (size_t)tile.group * r * sd.cols;
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    if (r0 + 16 * m >= r) break;
+    if (m0 + m >= tiles) break;
+    __syncthreads();
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -458,50 +711,87 @@ __global__ __launch_bounds__(kOuterWaves * 64) void outer_kernel(Outer o) {
             make_float4(acc[m][4 * h][e], acc[m][4 * h + 1][e], acc[m][4 * h + 2][e], acc[m][4 * h + 3][e]);
     __syncthreads();
     if (!sd.by_column) {
-      const int j = tid >> 5, n = (tid & 31) * 4;
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kOuterWaves; ++w) {
-        const float4 a = *reinterpret_cast<const float4*>(&red[w][j][n]);
-        sum.x += a.x; sum.y += a.y; sum.z += a.z; sum.w += a.w;
+      for (int k = 0; k < 2; ++k) {
+        const int jj = 8 * k + (tid >> 5), j = 16 * (m0 + m) + jj, n = (tid & 31) * 4;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kOuterWaves; ++w) {
+          const float4 a = *reinterpret_cast<const float4*>(&red[w][jj][n]);
+          sum.x += a.x; sum.y += a.y; sum.z += a.z; sum.w += a.w;
+        }
+        if (j < r && c0 + n < sd.cols)
+          *reinterpret_cast<float4*>(out + (size_t)j * sd.cols + c0 + n) =
+              make_float4(sum.x * scale, sum.y * scale, sum.z * scale, sum.w * scale);
       }
-      if (r0 + 16 * m + j < r && c0 + n < sd.cols)
-        *reinterpret_cast<float4*>(out + (size_t)(r0 + 16 * m + j) * sd.cols + c0 + n) =
-            make_float4(sum.x * scale, sum.y * scale, sum.z * scale, sum.w * scale);
     } else {
-      const int j = tid & 15;
 #pragma unroll
-      for (int h = 0; h < kOuterCols / 32; ++h) {
-        const int n = (tid >> 4) + 32 * h;
-        float sum = 0.f;
+      for (int k = 0; k < 2; ++k) {
+        const int n = 64 * k + (tid >> 2), jj = (tid & 3) * 4, j = 16 * (m0 + m) + jj;
+        float sum[4] = {};
 #pragma unroll
-        for (int w = 0; w < kOuterWaves; ++w) sum += red[w][j][n];
-        if (r0 + 16 * m + j < r && c0 + n < sd.cols) out[(size_t)(c0 + n) * r + r0 + 16 * m + j] = sum * scale;
+        for (int w = 0; w < kOuterWaves; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] += red[w][jj + i][n];
+        float* at = out + (size_t)(c0 + n) * r + j;
+        if (c0 + n < sd.cols) {
+          if ((r & 3) == 0) {
+            if (j < r) *reinterpret_cast<float4*>(at) = make_float4(sum[0] * scale, sum[1] * scale, sum[2] * scale, sum[3] * scale);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (j + i < r) at[i] = sum[i] * scale;
+          }
+        }
       }
     }
-    __syncthreads();
   }
 }
 
-// Adds the pieces of cut groups in order.  blockIdx.y: the group.
+// Adds the pieces of cut groups in order.  blockIdx.y: the group; four pieces in flight.
 static __global__ __launch_bounds__(256) void reduce_kernel(Outer o) {
   const int g = blockIdx.y;
-  const int first = o.rows.offsets != nullptr ? o.rows.offsets[g] : 0;
-  const int n = o.rows.offsets != nullptr ? o.rows.offsets[g + 1] - first : o.rows.T;
+  const int n = o.pieces != nullptr ? o.offsets[g + 1] - o.offsets[g] : o.T;
   if (n <= o.chunk) return;
-  const int slot = piece_slot(o.rows, o.chunk, Tile{g, first, n}), pieces = (n + o.chunk - 1) / o.chunk;
-  for (int s = 0; s < 2; ++s) {
-    const OuterSide& sd = o.side[s];
-    const size_t size = (size_t)o.r * sd.cols;  // (a multiple of 8)
-    for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (size_t)gridDim.x * 1024) {
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int p = 0; p < pieces; ++p) {
-        const float4 a = *reinterpret_cast<const float4*>(sd.part + (size_t)(slot + p) * size + i);
-        sum.x += a.x; sum.y += a.y; sum.z += a.z; sum.w += a.w;
-      }
-      *reinterpret_cast<float4*>(sd.out + (size_t)g * size + i) = sum;
+  const int slot = o.pieces != nullptr ? o.slot0[g] : 0, pieces = (n + o.chunk - 1) / o.chunk;
+  const size_t sizes[2] = {(size_t)o.r * o.side[0].cols, (size_t)o.r * o.side[1].cols};  // (multiples of 8)
+  for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < sizes[0] + sizes[1]; i += (size_t)gridDim.x * 1024) {
+    const bool second = i >= sizes[0];
+    const size_t size = second ? sizes[1] : sizes[0], at = second ? i - sizes[0] : i;
+    const float* part = (second ? o.side[1].part : o.side[0].part) + (size_t)slot * size + at;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < pieces; p += 4) {
+      float4 a[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[k] = *reinterpret_cast<const float4*>(part + (size_t)min(p + k, pieces - 1) * size);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (p + k < pieces) sum.x += a[k].x, sum.y += a[k].y, sum.z += a[k].z, sum.w += a[k].w;
     }
+    *reinterpret_cast<float4*>((second ? o.side[1].out : o.side[0].out) + (size_t)g * size + at) = sum;
   }
+}
+
+template <int MT>
+void launch_outer_tiles(const Outer& o, int pieces, hipStream_t s) {
+  hipLaunchKernelGGL(outer_kernel<MT>, dim3(o.side[0].tiles + o.side[1].tiles, pieces, ceil_div(o.r, 16 * MT)), dim3(kOuterThreads),
+                     0, s, o);
+}
+
+inline void launch_outer(const Outer& o, int pieces, bool cut, hipStream_t s) {
+  if (o.r <= 16) launch_outer_tiles<1>(o, pieces, s);
+  else if (o.r <= 32) launch_outer_tiles<2>(o, pieces, s);
+  else launch_outer_tiles<4>(o, pieces, s);
+  if (cut) {
+    const int64_t values = (int64_t)o.r * (o.side[0].cols + o.side[1].cols);
+    hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div(values, 1024), o.L), dim3(256), 0, s, o);
+  }
+}
+
+// Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.
+inline int outer_chunk(int T, int tiles, int r, int want) {
+  const int64_t chunk = ((int64_t)T * tiles * ceil_div(r, 64) / want + 255) / 256 * 256;
+  return chunk < 256 ? 256 : (chunk > kMaxChunk ? kMaxChunk : (int)chunk);
 }
 
 }  // namespace skinny
