@@ -126,7 +126,9 @@ __global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e)
     }
   __syncthreads();
   if (group < 0) {
-    copy_rows<YT>(e.y_in, e.y_out, e.keep, r, e.N, s_rows, n, blockIdx.x * kExpandWaves * 64, kExpandWaves * 64);
+    copy_rows<YT>(e.y_in, e.y_out, e.N, s_rows, n, blockIdx.x * kExpandWaves * 64, kExpandWaves * 64);
+    if (e.keep != nullptr && blockIdx.x == 0)
+      for (int i = tid; i < n * r; i += kExpandThreads) e.keep[(size_t)s_rows[i / r] * r + i % r] = 0.f;
     return;
   }
   const YT* in = static_cast<const YT*>(e.y_in);
@@ -233,9 +235,12 @@ struct Prepare {
   const int32_t* offsets;
   Pack pack;
 };
-__global__ __launch_bounds__(256) void prepare_kernel(Prepare p) {
-  __shared__ uint16_t s[64][66];
-  if (blockIdx.x >= (unsigned)(p.tiles * p.L)) return pack_block(p.pack, blockIdx.x - p.tiles * p.L);
+__global__ __launch_bounds__(kPackThreads) void prepare_kernel(Prepare p) {
+  __shared__ __align__(16) char s_buf[sizeof(PackBuffer)];
+  if (blockIdx.x >= (unsigned)(p.tiles * p.L))
+    return pack_block(p.pack, blockIdx.x - p.tiles * p.L, reinterpret_cast<float*>(s_buf), kPackStride);
+  uint16_t(*const s)[66] = reinterpret_cast<uint16_t(*)[66]>(s_buf);
+  static_assert(sizeof(PackBuffer) >= 64 * 66 * 2, "");
   const int g = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
   if (p.offsets[g] == p.offsets[g + 1]) return;
   const bool second = tile >= p.tiles_a;
@@ -243,35 +248,28 @@ __global__ __launch_bounds__(256) void prepare_kernel(Prepare p) {
   const int tc = second ? p.tiles_c[1] : p.tiles_c[0], r0 = b / tc * 64, c0 = b % tc * 64;
   const uint16_t* in = (second ? p.in[1] : p.in[0]) + (size_t)g * R * C;
   uint16_t* out = (second ? p.out[1] : p.out[0]) + (size_t)g * R * C;
+  static_assert(kPackThreads == 64 * 8, "eight lanes a row");
   const int i = threadIdx.x >> 3, j = (threadIdx.x & 7) * 8;
+  if (r0 + i < R && c0 + j < C) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(in + (size_t)(r0 + i) * C + c0 + j);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = r0 + i + 32 * h, c = c0 + j;
-    if (r < R && c < C) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(in + (size_t)r * C + c);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) s[i + 32 * h][j + k] = (uint16_t)(v[k / 2] >> (16 * (k & 1)));
-    }
+    for (int k = 0; k < 8; ++k) s[i][j + k] = (uint16_t)(v[k / 2] >> (16 * (k & 1)));
   }
   __syncthreads();
+  if (c0 + i < C && r0 + j < R) {
+    uint32_t v[4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int c = c0 + i + 32 * h, r = r0 + j;
-    if (c < C && r < R) {
-      uint32_t v[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = s[j + 2 * k][i + 32 * h] | (uint32_t)s[j + 2 * k + 1][i + 32 * h] << 16;
-      *reinterpret_cast<u32x4*>(out + (size_t)c * R + r) = u32x4{v[0], v[1], v[2], v[3]};
-    }
+    for (int k = 0; k < 4; ++k) v[k] = s[j + 2 * k][i] | (uint32_t)s[j + 2 * k + 1][i] << 16;
+    *reinterpret_cast<u32x4*>(out + (size_t)(c0 + i) * R + r0 + j) = u32x4{v[0], v[1], v[2], v[3]};
   }
 }
 
 // How a call is cut, and its workspace in order: a function of its sizes.
 struct Plan {
   bool few;
-  int shrink_rows, n_shrink, n_expand, split;
+  int n_tiles, slices;
   int chunk, n_pieces, slots;  // backward: rows per piece of the outer products, pieces, partial results of cut groups
-  size_t offsets, list, shrink, expand, pieces, piece_slots, slot0, part, packed, at, bt, outer_u, outer_v, partial, bytes;
+  size_t offsets, list, tiles, pieces, piece_slots, slot0, part, packed, at, bt, outer_u, outer_v, partial, bytes;
 };
 
 Plan make_plan(int T, int K, int N, int rank, int L, bool backward) {
@@ -283,21 +281,17 @@ Plan make_plan(int T, int K, int N, int rank, int L, bool backward) {
     return here;
   };
   p.few = !backward && T <= kFewRows;
+  p.slices = p.few ? few_pieces(K) : (T > 0 ? shrink_slices(T, backward ? N : K) : 1);
+  p.part = take((size_t)p.slices * T * rank * sizeof(float));
   if (p.few) {
-    p.part = take((size_t)few_pieces(K) * T * rank * sizeof(float));
     p.bytes = at > 0 ? at : 256;
     return p;
   }
-  // tiles of 32 rows once those of 16 are more than the compute units (M_a is read for each of them); outer products want 32
-  p.shrink_rows = backward || T > 6144 ? 32 : 16;
-  p.split = 3;  // (two parts for bf16 results)
-  p.n_shrink = (max_tiles(T, L, p.shrink_rows) + 7) / 8 * 8;
-  p.n_expand = max_tiles(T, L + 1, kExpandRows);
+  p.n_tiles = max_tiles(T, L + 1);
   p.offsets = take((L + 2) * sizeof(int32_t));
   p.list = take((size_t)T * sizeof(int32_t));
-  p.shrink = take(p.n_shrink * sizeof(Tile));
-  p.expand = take(p.n_expand * sizeof(Tile));
-  p.packed = take(packed_bytes(p.n_shrink * (p.shrink_rows / 16), rank, p.split));
+  p.tiles = take(p.n_tiles * sizeof(Tile));
+  p.packed = take(packed_bytes(p.n_tiles, rank, 3));  // (two parts for bf16 results)
   if (backward) {
     p.chunk = outer_chunk(T, ceil_div(K, kOuterCols) + ceil_div(N, kOuterCols), rank, 512);
     p.n_pieces = T / p.chunk + L;
@@ -307,8 +301,8 @@ Plan make_plan(int T, int K, int N, int rank, int L, bool backward) {
     p.slot0 = take(L * sizeof(int32_t));
     p.at = take((size_t)L * K * rank * 2);
     p.bt = take((size_t)L * N * rank * 2);
-    p.outer_u = take(outer_bytes(p.n_shrink, rank));
-    p.outer_v = take(outer_bytes(p.n_shrink, rank));
+    p.outer_u = take(outer_bytes(p.n_tiles, rank));
+    p.outer_v = take(outer_bytes(p.n_tiles, rank));
     p.partial = take((size_t)p.slots * rank * ((size_t)K + N) * sizeof(float));
   }
   p.bytes = at;
@@ -321,9 +315,8 @@ T* at(char* ws, size_t offset) {
 }
 
 void launch_sort(const Plan& p, const int32_t* idx, int T, int L, char* ws, hipStream_t s) {
-  const Sort sort{idx, T, L, p.shrink_rows, p.chunk, p.n_shrink, p.n_expand, p.n_pieces, at<int32_t>(ws, p.offsets),
-                  at<int32_t>(ws, p.list), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0), at<Tile>(ws, p.shrink),
-                  at<Tile>(ws, p.expand), at<Tile>(ws, p.pieces)};
+  const Sort sort{idx, T, L, p.chunk, p.n_tiles, p.n_pieces, at<int32_t>(ws, p.offsets), at<int32_t>(ws, p.list),
+                  at<Tile>(ws, p.tiles), at<Tile>(ws, p.pieces), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0)};
   hipLaunchKernelGGL(sort_kernel, dim3(1), dim3(kSortThreads), 0, s, sort);
 }
 
@@ -369,18 +362,21 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
     const Few few{adapter_idx, T, n_adapters};
     float* const part = at<float>(ws, p.part);
     launch_shrink_few(few, x, K, a, rank, part, s);
-    const ExpandFew e{few, part, few_pieces(K), rank, scale, v, b, N, y_in, y_out};
+    const ExpandFew e{few, part, p.slices, rank, scale, v, b, N, y_in, y_out};
     if (f32) launch_expand_few<float, 3>(e, s);
     else launch_expand_few<uint16_t, 2>(e, s);
   } else {
     launch_sort(p, adapter_idx, T, n_adapters, ws, s);
     const int32_t* list = at<int32_t>(ws, p.list);
+    const Tile* tiles = at<Tile>(ws, p.tiles);
+    float* const part = at<float>(ws, p.part);
     u32x4* const packed = at<u32x4>(ws, p.packed);
-    launch_shrink(Shrink{at<Tile>(ws, p.shrink), list, x, a, K, rank, f32 ? 3 : 2, scale, v, packed, nullptr}, p.n_shrink,
-                  p.shrink_rows, s);
-    const Expand e{at<Tile>(ws, p.expand), list, T, n_adapters, packed, rank, b, rank, N, y_in, y_out, v};
-    if (f32) launch_expand<float, 3>(e, p.n_expand, s);
-    else launch_expand<uint16_t, 2>(e, p.n_expand, s);
+    launch_shrink(Shrink{tiles, list, T, n_adapters, x, a, K, rank, part}, p.n_tiles, p.slices, s);
+    hipLaunchKernelGGL(pack_kernel, dim3(2 * p.n_tiles), dim3(kPackThreads), 0, s,
+                       Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, v, f32 ? 3 : 2, packed, nullptr});
+    const Expand e{tiles, list, T, n_adapters, packed, rank, b, rank, N, y_in, y_out};
+    if (f32) launch_expand<float, 3>(e, p.n_tiles, s);
+    else launch_expand<uint16_t, 2>(e, p.n_tiles, s);
   }
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
@@ -407,20 +403,23 @@ int moe_lora_backward(const void* x_bf16, const void* dy_bf16, const int32_t* ad
   char* const ws = static_cast<char*>(workspace);
   launch_sort(p, adapter_idx, T, n_adapters, ws, s);
   const int32_t *list = at<int32_t>(ws, p.list), *offsets = at<int32_t>(ws, p.offsets);
-  const Tile* tiles = at<Tile>(ws, p.shrink);
+  const Tile* tiles = at<Tile>(ws, p.tiles);
   u32x4 *const outer_u = at<u32x4>(ws, p.outer_u), *const outer_v = at<u32x4>(ws, p.outer_v);
   if (T > 0) {
     const int ra = ceil_div(rank, 64), ca = ceil_div(K, 64), cb = ceil_div(N, 64);
     uint16_t *const a_t = at<uint16_t>(ws, p.at), *const b_t = at<uint16_t>(ws, p.bt);
     const Prepare prep{{static_cast<const uint16_t*>(lora_a), static_cast<const uint16_t*>(lora_b)}, {a_t, b_t}, {rank, N}, {K, rank},
                        {ca, ra}, ra * ca, ra * (ca + cb), n_adapters, offsets,
-                       Pack{tiles, list, T, v, rank, nullptr, outer_v}};
-    hipLaunchKernelGGL(prepare_kernel, dim3(prep.tiles * n_adapters + p.n_shrink), dim3(256), 0, s, prep);
+                       Pack{tiles, list, T, n_adapters, v, 1, rank, true, nullptr, nullptr, 0, nullptr, outer_v}};
+    hipLaunchKernelGGL(prepare_kernel, dim3(prep.tiles * n_adapters + 2 * p.n_tiles), dim3(kPackThreads), 0, s, prep);
+    float* const part = at<float>(ws, p.part);
     u32x4* const packed = at<u32x4>(ws, p.packed);
-    launch_shrink(Shrink{tiles, list, dy, b_t, N, rank, 2, scale, nullptr, packed, outer_u}, p.n_shrink, p.shrink_rows, s);
+    launch_shrink(Shrink{tiles, list, T, n_adapters, dy, b_t, N, rank, part}, p.n_tiles, p.slices, s);
+    hipLaunchKernelGGL(pack_kernel, dim3(2 * p.n_tiles), dim3(kPackThreads), 0, s,
+                       Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, nullptr, 2, dx != nullptr ? packed : nullptr,
+                            outer_u});
     if (dx != nullptr)
-      launch_expand<uint16_t, 2>(Expand{at<Tile>(ws, p.expand), list, T, n_adapters, packed, rank, a_t, rank, K, dx_in, dx, nullptr},
-                                 p.n_expand, s);
+      launch_expand<uint16_t, 2>(Expand{tiles, list, T, n_adapters, packed, rank, a_t, rank, K, dx_in, dx}, p.n_tiles, s);
   }
   float* const partial = at<float>(ws, p.partial);
   const Outer o{at<Tile>(ws, p.pieces), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0), offsets, list, T, n_adapters,

@@ -267,13 +267,15 @@ struct LaunchRoute {
 // columns, E rounded up to a multiple of 32 by zeros.
 int router_width(int E) { return ceil_div(E, 32) * 32; }
 
-// In one launch: W_r's parts, 1024 values a workgroup, and d_logits' fragments, 32 rows a workgroup.
-__global__ __launch_bounds__(kThreads) void router_prepare_kernel(const float* __restrict__ w, int64_t n, int E, int R,
-                                                                  uint16_t* __restrict__ out, int split_blocks, Pack pack) {
-  if (blockIdx.x >= (unsigned)split_blocks) return pack_block(pack, blockIdx.x - split_blocks);
+// In one launch: W_r's parts, 2048 values a workgroup, and d_logits' fragments, 32 rows a workgroup.
+constexpr int kSplitValues = 4;
+__global__ __launch_bounds__(kPackThreads) void router_prepare_kernel(const float* __restrict__ w, int64_t n, int E, int R,
+                                                                      uint16_t* __restrict__ out, int split_blocks, Pack pack) {
+  __shared__ __align__(16) float s_sum[32][kMaxGroups + 4];
+  if (blockIdx.x >= (unsigned)split_blocks) return pack_block(pack, blockIdx.x - split_blocks, &s_sum[0][0], kMaxGroups + 4);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int64_t i = (int64_t)blockIdx.x * 4 * kThreads + k * kThreads + threadIdx.x;
+  for (int k = 0; k < kSplitValues; ++k) {
+    const int64_t i = ((int64_t)blockIdx.x * kSplitValues + k) * kPackThreads + threadIdx.x;
     if (i >= n) break;
     const int64_t h = i / R;
     const int e = (int)(i - h * R);
@@ -285,18 +287,18 @@ __global__ __launch_bounds__(kThreads) void router_prepare_kernel(const float* _
 }
 
 struct RouterPlan {
-  int chunk, pieces, slots, blocks;
+  int chunk, pieces, slots, tiles;
   size_t split, packed, outer, partial, bytes;  // offsets in the workspace
 };
 RouterPlan plan_router(int T, int H, int E) {
   RouterPlan p = {};
-  p.chunk = outer_chunk(T, ceil_div(H, kOuterCols), E, 256);
+  p.chunk = outer_chunk(T, ceil_div(H, kOuterCols), E, 512);
   p.pieces = T > p.chunk ? ceil_div(T, p.chunk) : 1;
   p.slots = T > p.chunk ? p.pieces : 0;
-  p.blocks = ceil_div(T, 32);
+  p.tiles = ceil_div(T, kTileRows);
   p.packed = padded((size_t)H * 2 * router_width(E) * 2);
-  p.outer = p.packed + padded(packed_bytes(2 * p.blocks, E, 2));
-  p.partial = p.outer + padded(outer_bytes(p.blocks, E));
+  p.outer = p.packed + padded(packed_bytes(p.tiles, E, 2));
+  p.partial = p.outer + padded(outer_bytes(p.tiles, E));
   p.bytes = p.partial + padded((size_t)p.slots * H * E * sizeof(float));
   return p;
 }
@@ -460,9 +462,11 @@ int moe_router_backward(const void* x_bf16, const float* w_router, const float* 
   uint16_t* const split = reinterpret_cast<uint16_t*>(ws + p.split);
   u32x4 *const packed = reinterpret_cast<u32x4*>(ws + p.packed), *const outer = reinterpret_cast<u32x4*>(ws + p.outer);
   if (T > 0) {
-    const int split_blocks = dx != nullptr ? ceil_div((int64_t)H * R, 4 * kThreads) : 0;
-    hipLaunchKernelGGL(router_prepare_kernel, dim3(split_blocks + p.blocks), dim3(kThreads), 0, s, w_router, (int64_t)H * R, E, R, split,
-                       split_blocks, Pack{nullptr, nullptr, T, d_logits, E, dx != nullptr ? packed : nullptr, outer});
+    const int split_blocks = dx != nullptr ? ceil_div((int64_t)H * R, kSplitValues * kPackThreads) : 0;
+    hipLaunchKernelGGL(router_prepare_kernel, dim3(split_blocks + 2 * p.tiles), dim3(kPackThreads), 0, s, w_router, (int64_t)H * R, E, R, split,
+                       split_blocks,
+                       Pack{nullptr, nullptr, T, 1, d_logits, 1, E, E % 4 == 0 && aligned16(d_logits), nullptr, nullptr, 2,
+                            dx != nullptr ? packed : nullptr, outer});
   }
   const Outer o{nullptr, nullptr, nullptr, nullptr, nullptr, T, 1,
                 {{static_cast<const uint16_t*>(x_bf16), outer, nullptr, d_w_router, reinterpret_cast<float*>(ws + p.partial), H,
@@ -471,8 +475,8 @@ int moe_router_backward(const void* x_bf16, const float* w_router, const float* 
                 E, p.chunk};
   launch_outer(o, p.pieces, p.slots > 0, s);
   if (dx != nullptr && T > 0) {
-    const Expand e{nullptr, nullptr, T, 1, packed, E, split, 2 * R, H, dx_in, dx, nullptr};
-    const int tiles = ceil_div(T, kExpandRows);
+    const Expand e{nullptr, nullptr, T, 1, packed, E, split, 2 * R, H, dx_in, dx};
+    const int tiles = p.tiles;
     // M_a's fragments in registers: fewer columns a wavefront for more experts
     if (R == 32) launch_expand_kernel<uint16_t, 2, 2, 1, 8>(e, tiles, s);
     else if (R == 64) launch_expand_kernel<uint16_t, 2, 2, 2, 8>(e, tiles, s);

@@ -57,28 +57,23 @@ inline size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 struct Tile {
   int32_t group, first, rows, at;  // first: position in the list; rows 0: nothing to do
 };
-struct Work {
-  const int32_t* offsets;  // [L+2]
-  const int32_t* list;     // positions -> rows
-  const Tile* shrink;      // tiles of shrink_rows; at: their number in the order of the groups
-  const Tile* expand;      // tiles of kExpandRows; at: the number of their first 16 rows
-  const Tile* pieces;      // of up to `chunk` rows, one at least for each group; at: the number of their first 32 rows (shrink_rows == 32)
-  const int32_t* slots;    // the place of a piece's partial result, -1: its group is not cut
-  const int32_t* slot0;    // [L] that of a group's first piece
-};
-constexpr int kExpandRows = 64;
+constexpr int kTileRows = 64;
 
-// Tiles of M rows that T rows in at most L groups can have.
-inline int max_tiles(int T, int L, int M) { return T / M + (L < T ? L : T); }
+// Tiles of kTileRows rows that T rows in at most L groups can have.
+inline int max_tiles(int T, int L) { return T / kTileRows + (L < T ? L : T); }
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave, kMaxGroups = 256;
 
 struct Sort {
   const int32_t* idx;
-  int T, L, shrink_rows, chunk;         // chunk 0: no pieces
-  int n_shrink, n_expand, n_pieces;     // entries of the lists
-  int32_t *offsets, *list, *slots, *slot0;
-  Tile *shrink, *expand, *pieces;
+  int T, L, chunk;           // chunk: rows of a piece, 0: none are listed
+  int n_tiles, n_pieces;     // entries of the lists
+  int32_t* offsets;          // [L+2] first position of each group in `list`
+  int32_t* list;             // [T] positions -> rows
+  Tile* tiles;               // of kTileRows rows; at: their number
+  Tile* pieces;              // of up to `chunk` rows, one at least for each group < L; at: the number of their first 32 rows
+  int32_t* slots;            // the place of a piece's partial result, -1: its group is not cut
+  int32_t* slot0;            // [L] that of a group's first piece
 };
 
 // Rank of this lane among the lanes of its wavefront with the same group, and how many there are: a ballot for each bit of the id.
@@ -108,7 +103,7 @@ __device__ __forceinline__ int find_group(const int32_t* pre, int n, int v) {
 // steps, which cost more until there are some ten thousand rows; beyond, the products take longer by far.)
 static __global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
   __shared__ int32_t cnt[kSortWaves][kMaxGroups + 1];
-  __shared__ int32_t pre[5][kMaxGroups + 2];  // prefixes over the groups of rows, shrink tiles, expand tiles, pieces, slots
+  __shared__ int32_t pre[4][kMaxGroups + 2];  // prefixes over the groups of rows, tiles, pieces, slots
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, groups = s.L + 1, bits = 32 - __clz(s.L);
   const int share = ((s.T + kSortWaves - 1) / kSortWaves + kWave - 1) / kWave * kWave;
   const int t0 = min(wave * share, s.T), t1 = min(t0 + share, s.T);
@@ -152,18 +147,17 @@ static __global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
   }
   __syncthreads();
   if (wave == 0) {
-    int carry[5] = {};
+    int carry[4] = {};
     for (int g0 = 0; g0 < groups; g0 += kWave) {
       const int g = g0 + lane;
-      const bool own = g < s.L;
       const int c = g < groups ? pre[0][g] : 0;
-      int v[5] = {c, own ? (c + s.shrink_rows - 1) / s.shrink_rows : 0, (c + kExpandRows - 1) / kExpandRows, 0, 0};
-      if (s.chunk > 0 && own) {
-        v[3] = max(1, (c + s.chunk - 1) / s.chunk);
-        v[4] = c > s.chunk ? v[3] : 0;
+      int v[4] = {c, (c + kTileRows - 1) / kTileRows, 0, 0};
+      if (s.chunk > 0 && g < s.L) {
+        v[2] = max(1, (c + s.chunk - 1) / s.chunk);
+        v[3] = c > s.chunk ? v[2] : 0;
       }
 #pragma unroll
-      for (int k = 0; k < 5; ++k) {
+      for (int k = 0; k < 4; ++k) {
         const int incl = gg::wave_incl_scan(v[k]);
         if (g < groups) pre[k][g] = carry[k] + incl - v[k];
         carry[k] += (int)__builtin_amdgcn_readlane(incl, kWave - 1);
@@ -171,7 +165,7 @@ static __global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
     }
     if (lane == 0)
 #pragma unroll
-      for (int k = 0; k < 5; ++k) pre[k][groups] = carry[k];
+      for (int k = 0; k < 4; ++k) pre[k][groups] = carry[k];
   }
   __syncthreads();
   for (int g = tid; g <= groups; g += kSortThreads) s.offsets[g] = pre[0][g];
@@ -190,62 +184,53 @@ static __global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
       if (in && rank == 0) cnt[wave][g[u]] += n;
     }
   }
-  // the lists: neighbours in the order of the groups run on one XCD (workgroups b, b + 8, ...), whose L2 then holds few groups' matrices
-  for (int i = tid; i < s.n_shrink + s.n_expand + s.n_pieces; i += kSortThreads) {
-    int b = i, kind = 1;
-    if (i >= s.n_shrink + s.n_expand) b = i - s.n_shrink - s.n_expand, kind = 3;
-    else if (i >= s.n_shrink) b = i - s.n_shrink, kind = 2;
-    int at = b, total = pre[kind][groups];
-    if (kind == 1) {
-      const int per = (total + 7) / 8;
-      b = b / 8 < per ? b % 8 * per + b / 8 : total;
-    }
-    Tile t{kind == 3 ? -1 : 0, 0, 0, 0};
+  for (int i = tid; i < s.n_tiles + s.n_pieces; i += kSortThreads) {
+    const bool tile = i < s.n_tiles;
+    const int b = tile ? i : i - s.n_tiles, kind = tile ? 1 : 2, rows = tile ? kTileRows : s.chunk;
+    Tile t{-1, 0, 0, 0};
     int slot = -1;
-    if (b < total) {
+    if (b < pre[kind][groups]) {
       const int g = find_group(pre[kind], groups, b), p = b - pre[kind][g], n = pre[0][g + 1] - pre[0][g];
-      const int rows = kind == 1 ? s.shrink_rows : (kind == 2 ? kExpandRows : s.chunk), k = p * rows;
-      t = Tile{g, pre[0][g] + k, min(rows, n - k), kind == 1 ? b : (pre[1][g] * s.shrink_rows + k) / (kind == 2 ? 16 : 32)};
-      if (kind == 3) {
-        if (n > s.chunk) slot = pre[4][g] + p;
+      t = Tile{g, pre[0][g] + p * rows, min(rows, n - p * rows), tile ? b : pre[1][g] * (kTileRows / 32) + p * rows / 32};
+      if (!tile) {
+        if (n > s.chunk) slot = pre[3][g] + p;
         if (p == 0) s.slot0[g] = slot;
       }
     }
-    (kind == 1 ? s.shrink : (kind == 2 ? s.expand : s.pieces))[at] = t;
-    if (kind == 3) s.slots[at] = slot;
+    if (tile) s.tiles[b] = t;
+    else s.pieces[b] = t, s.slots[b] = slot;
   }
 }
 
 // ---- shrink ------------------------------------------------------------------------------------------------------------------
-// A workgroup of 8 wavefronts computes the sums of 16 MT rows, so that they need not be joined by another kernel; a wavefront takes its
-// 8th of k in pieces of 64: 128 bytes of each row, read by eight neighbouring lanes, put into the wavefront's own piece of LDS with the
-// 16-byte parts of a row rearranged by the row's number, and read back as fragments without bank conflicts.  The next U pieces of x are on
-// their way from HBM meanwhile, and the next 32 rows of M_a from L2.  The wavefronts' sums are added in order through LDS.  Tiles begin
-// their walk apart, so that the rows' pieces that the chip reads at one time, a power of two apart in memory, are not those of a
-// few memory channels.
-constexpr int kShrinkWaves = 8, kShrinkThreads = kShrinkWaves * 64;
+// A workgroup of 4 wavefronts computes one slice (blockIdx.y) of the sum for 64 rows, a wavefront a quarter of the slice in pieces of 64:
+// 128 bytes of each row, read by eight neighbouring lanes, put into the wavefront's own piece of LDS with the 16-byte parts of a row
+// rearranged by the row's number, and read back as fragments without bank conflicts.  The next piece of x is on its way from HBM
+// meanwhile, and the next 32 rows of M_a from L2.  The wavefronts' sums are added in order through LDS, the slices' by pack_kernel.
+// Why slices: a compute unit takes in about 45 KB a microsecond whatever the pattern, so what counts is how many bytes the busiest one
+// reads.  With 16 rows of all of k a workgroup, M_a would be twice x's bytes at rank 32, and 260 workgroups on 256 units took half as
+// long again as 256 (19 and 12.6 us; 33 MB of x).
+constexpr int kShrinkWaves = 4, kShrinkThreads = kShrinkWaves * 64;
 
 struct Shrink {
   const Tile* tiles;
   const int32_t* list;
+  int T, L;
   const uint16_t* x;  // [T][K]
   const uint16_t* m;  // [L][r][K]
-  int K, r, split;
-  const float* scale;  // per group, for `packed` and `outer`
-  float* keep;         // [T][r] the sums as they are, or nullptr
-  u32x4* packed;       // for expand: [tiles of 16 rows][chunks of 32 columns][split][64]
-  u32x4* outer;        // for outer: [tiles of 32 rows][tiles of 16 columns][3][64], or nullptr (MT == 2 only)
+  int K, r;
+  float* part;        // [slices][T][r]
 };
 
-template <int MT, int NT>
-__global__ __launch_bounds__(kShrinkThreads, MT * NT > 8 ? 2 : 4) void shrink_kernel(Shrink a) {
-  constexpr int M = 16 * MT, NG = NT < 2 ? NT : 2, GROUPS = NT / NG, U = MT * NT >= 8 ? 1 : (MT * NT <= 2 ? 4 : 2);
-  constexpr int kWaveBytes = (M + 16 * NG) * 128, kRedStride = NT * 16 + 1, kCols = NT < 2 ? 32 : NT * 16, kSumStride = kCols + 4;
-  constexpr int kRedBytes = kShrinkWaves * 16 * kRedStride * 4, kSumBytes = M * kSumStride * 4, kBytes = kShrinkWaves * kWaveBytes;
+template <int NT>
+__global__ __launch_bounds__(kShrinkThreads, 2) void shrink_kernel(Shrink a) {
+  constexpr int M = kTileRows, MT = M / 16, NG = NT < 2 ? NT : 2, GROUPS = NT / NG;
+  constexpr int kWaveBytes = (M + 16 * NG) * 128, kRedStride = NT * 16 + 4, kRound = NT <= 2 ? 64 : 128 / NT;  // rows joined at a time
+  constexpr int kRedBytes = kShrinkWaves * kRound * kRedStride * 4, kBytes = kShrinkWaves * kWaveBytes;
   __shared__ int32_t s_rows[M];
-  __shared__ __align__(16) char s_buf[kBytes > kRedBytes + kSumBytes ? kBytes : kRedBytes + kSumBytes];
+  __shared__ __align__(16) char s_buf[kBytes > kRedBytes ? kBytes : kRedBytes];
   const Tile tile = a.tiles[blockIdx.x];
-  if (tile.rows == 0) return;
+  if (tile.rows == 0 || tile.group == a.L) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, q = lane >> 4, sub = lane >> 3, ch = lane & 7;
   const int K = a.K, r = a.r;
   if (tid < M) s_rows[tid] = a.list[tile.first + min(tid, tile.rows - 1)];
@@ -261,174 +246,196 @@ __global__ __launch_bounds__(kShrinkThreads, MT * NT > 8 ? 2 : 4) void shrink_ke
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int pieces = (K + 63) / 64, first = pieces * wave / kShrinkWaves, n = pieces * (wave + 1) / kShrinkWaves - first;
+  const int pieces = (K + 63) / 64, parts = kShrinkWaves * gridDim.y, w = blockIdx.y * kShrinkWaves + wave;
+  const int first = pieces * w / parts, n = pieces * (w + 1) / parts - first;
   // Straight-line code: a load under a condition makes the compiler wait for all loads.  Past the end the last piece is loaded again,
-  // past K the first columns, and x's part set to zero.
-  u32x4 xv[U][2 * MT], mv[2 * NG];
-  const int turn = n > 0 ? tile.at % n : 0;
-  const auto piece = [&](int i) {
-    i = min(i, n - 1) + turn;
-    return (first + (i < n ? i : i - n)) * 64;
-  };
-  const auto load_x = [&](u32x4(&v)[2 * MT], int c) {
+  // past K the first columns, and x's part set to zero.  Loads return in the order they are issued in, so M_a's go first.
+  u32x4 xv[2 * MT], mv[2 * NG];
+  const auto load_x = [&](int i) {
+    int c = (first + min(i, n - 1)) * 64;
     c = c + 8 * ch < K ? c : -8 * ch;  // (K is a multiple of 8)
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) v[i] = *reinterpret_cast<const u32x4*>(xr[i] + c);
+    for (int k = 0; k < 2 * MT; ++k) xv[k] = *reinterpret_cast<const u32x4*>(xr[k] + c);
   };
-  const auto load_m = [&](int c, int g) {
+  const auto load_m = [&](int i, int g) {
+    int c = (first + min(i, n - 1)) * 64;
     c = c + 8 * ch < K ? c : -8 * ch;
 #pragma unroll
-    for (int i = 0; i < 2 * NG; ++i) mv[i] = *reinterpret_cast<const u32x4*>(mg + (size_t)min(32 * g + 8 * i + sub, r - 1) * K + c);
+    for (int k = 0; k < 2 * NG; ++k) mv[k] = *reinterpret_cast<const u32x4*>(mg + (size_t)min(32 * g + 8 * k + sub, r - 1) * K + c);
   };
   if (n > 0) {
-    load_m(piece(0), 0);
+    load_m(0, 0);
+    load_x(0);
+  }
+  for (int i = 0; i < n; ++i) {
+    const bool in = (first + i) * 64 + 8 * ch < K;
 #pragma unroll
-    for (int u = 0; u < U; ++u) load_x(xv[u], piece(u));
-    for (int i0 = 0; i0 < n; i0 += U) {
+    for (int k = 0; k < 2 * MT; ++k) {
+      const u32x4 v = xv[k];
+      *reinterpret_cast<u32x4*>(s_x + put + 1024 * k) = u32x4{in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u};
+    }
+    u32x4 f[MT][2];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + u;
-        const bool in = i < n && piece(i) + 8 * ch < K;
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int k = 0; k < 2 * MT; ++k) {
-          const u32x4 v = xv[u][k];
-          *reinterpret_cast<u32x4*>(s_x + put + 1024 * k) = u32x4{in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u};
-        }
-        u32x4 f[MT][2];
+      for (int h = 0; h < 2; ++h)
+        f[t][h] = *reinterpret_cast<const u32x4*>(s_x + (16 * t + ln) * 128 + (((4 * h + q) ^ (ln & 7)) * 16));
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+    for (int g = 0; g < GROUPS; ++g) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            f[t][h] = *reinterpret_cast<const u32x4*>(s_x + (16 * t + ln) * 128 + (((4 * h + q) ^ (ln & 7)) * 16));
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-#pragma unroll
-          for (int k = 0; k < 2 * NG; ++k) *reinterpret_cast<u32x4*>(s_m + put + 1024 * k) = mv[k];
-          if (g + 1 < GROUPS) load_m(piece(i), g + 1);
-          else {  // M_a's first: loads return in order, and it is waited for first
-            load_m(piece(i + 1), 0);
-            __builtin_amdgcn_sched_barrier(0);
-            load_x(xv[u], piece(i + U));
-          }
-#pragma unroll
-          for (int j = 0; j < NG; ++j)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const u32x4 b = *reinterpret_cast<const u32x4*>(s_m + (16 * j + ln) * 128 + (((4 * h + q) ^ (ln & 7)) * 16));
-#pragma unroll
-              for (int t = 0; t < MT; ++t) acc[t][g * NG + j] = mfma(f[t][h], b, acc[t][g * NG + j]);
-            }
-        }
+      for (int k = 0; k < 2 * NG; ++k) *reinterpret_cast<u32x4*>(s_m + put + 1024 * k) = mv[k];
+      if (g + 1 < GROUPS) load_m(i, g + 1);
+      else {
+        load_m(i + 1, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        load_x(i + 1);
       }
+#pragma unroll
+      for (int j = 0; j < NG; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const u32x4 b = *reinterpret_cast<const u32x4*>(s_m + (16 * j + ln) * 128 + (((4 * h + q) ^ (ln & 7)) * 16));
+#pragma unroll
+          for (int t = 0; t < MT; ++t) acc[t][g * NG + j] = mfma(f[t][h], b, acc[t][g * NG + j]);
+        }
     }
   }
-  float* const red = reinterpret_cast<float*>(s_buf);              // [wave][16][kRedStride]
-  float* const sum = reinterpret_cast<float*>(s_buf + kRedBytes);  // [M][kSumStride], zeros past the rows and past r
+  float* const red = reinterpret_cast<float*>(s_buf);  // [wave][kRound][kRedStride]
+  float* const part = a.part + (size_t)blockIdx.y * a.T * r;
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
+  for (int t0 = 0; t0 < M; t0 += kRound) {
+    if (t0 >= tile.rows) break;
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int t = 0; t < kRound / 16; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) red[(wave * 16 + 4 * q + e) * kRedStride + 16 * j + ln] = acc[t][j][e];
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          red[(wave * kRound + 16 * t + 4 * q + e) * kRedStride + 16 * j + ln] = acc[t0 / 16 + t][j][e];
     __syncthreads();
-    for (int o = tid; o < 16 * kCols; o += kShrinkThreads) {
-      const int ro = o / kCols, col = o % kCols;
-      float v = 0.f;
-      if (16 * t + ro < tile.rows && col < r) {
 #pragma unroll
-        for (int w = 0; w < kShrinkWaves; ++w) v += red[(w * 16 + ro) * kRedStride + col];
-        if (a.keep != nullptr) a.keep[(size_t)s_rows[16 * t + ro] * r + col] = v;
+    for (int o = tid; o < kRound * 4 * NT; o += kShrinkThreads) {
+      const int ro = o / (4 * NT), col = o % (4 * NT) * 4;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kShrinkWaves; ++w) {
+        const float4 p = *reinterpret_cast<const float4*>(red + (w * kRound + ro) * kRedStride + col);
+        v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
       }
-      sum[(16 * t + ro) * kSumStride + col] = v;
+      if (t0 + ro < tile.rows && col < r) *reinterpret_cast<float4*>(part + (size_t)s_rows[t0 + ro] * r + col) = v;
     }
+  }
+}
+
+// Slices of the sum: about 512 workgroups, two pieces of 64 for each wavefront at least, 8 slices (which pack_kernel reads at once) at most.
+inline int shrink_slices(int T, int K) {
+  int n = ceil_div(512, ceil_div(T, kTileRows));
+  const int most = ceil_div(K, 64 * 2 * kShrinkWaves);
+  if (n > most) n = most;
+  return n < 8 ? n : 8;
+}
+
+inline void launch_shrink(const Shrink& a, int n_tiles, int slices, hipStream_t s) {
+  const dim3 grid(n_tiles, slices), block(kShrinkThreads);
+  if (a.r <= 16) hipLaunchKernelGGL(shrink_kernel<1>, grid, block, 0, s, a);
+  else if (a.r <= 32) hipLaunchKernelGGL(shrink_kernel<2>, grid, block, 0, s, a);
+  else if (a.r <= 64) hipLaunchKernelGGL(shrink_kernel<4>, grid, block, 0, s, a);
+  else hipLaunchKernelGGL(shrink_kernel<8>, grid, block, 0, s, a);
+}
+
+// ---- pack --------------------------------------------------------------------------------------------------------------------
+// P from its slices, added in order, in the forms that the products read: a wavefront's 64 lanes one after the other, 16 bytes each.
+// 32 rows a workgroup: half a tile.
+struct Pack {
+  const Tile* tiles;    // nullptr: all rows one group
+  const int32_t* list;
+  int T, L;
+  const float* part;    // [slices][T][r]
+  int slices, r;
+  bool vec;             // rows of `part` are made of whole 16-byte pieces
+  const float* scale;   // per group, for `packed` and `outer`; or nullptr
+  float* keep;          // [T][r] the sums as they are, zeros for rows without a group; or nullptr
+  int split;            // parts of `packed`
+  u32x4* packed;        // for expand: [tiles][4][chunks of 32 columns][split][64]; or nullptr
+  u32x4* outer;         // for outer: [tiles][2][tiles of 16 columns][3][64]; or nullptr
+};
+constexpr int kPackThreads = 512, kPackStride = 132;
+typedef float PackBuffer[32][kPackStride];
+
+__device__ __forceinline__ void pack_block(const Pack& a, int b, float* s_sum, int stride) {
+  const int tid = threadIdx.x, half = b & 1;
+  Tile t{0, (b >> 1) * kTileRows, 0, b >> 1};
+  if (a.tiles != nullptr) t = a.tiles[b >> 1];
+  else t.rows = min(kTileRows, a.T - t.first);
+  const int rows = min(32, t.rows - 32 * half), first = t.first + 32 * half, r = a.r;
+  if (rows <= 0) return;
+  const auto row_of = [&](int i) { return a.list != nullptr ? a.list[first + i] : first + i; };
+  if (t.group == a.L) {
+    if (a.keep != nullptr)
+      for (int o = tid; o < rows * r; o += kPackThreads) a.keep[(size_t)row_of(o / r) * r + o % r] = 0.f;
+    return;
+  }
+  const int chunks = (r + 31) / 32, cols = 32 * chunks;
+  const size_t slice = (size_t)a.T * r;
+  for (int o = tid; o < 32 * cols / 4; o += kPackThreads) {  // four values
+    const int i = o / (cols / 4), j = o % (cols / 4) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < rows && j < r) {
+      const size_t at = (size_t)row_of(i) * r + j;
+      if (a.vec) {
+        for (int s0 = 0; s0 < a.slices; s0 += 8) {
+          float4 p[8];
+#pragma unroll
+          for (int s = 0; s < 8; ++s) p[s] = *reinterpret_cast<const float4*>(a.part + min(s0 + s, a.slices - 1) * slice + at);
+#pragma unroll
+          for (int s = 0; s < 8; ++s)
+            if (s0 + s < a.slices) v.x += p[s].x, v.y += p[s].y, v.z += p[s].z, v.w += p[s].w;
+        }
+        if (a.keep != nullptr) *reinterpret_cast<float4*>(a.keep + at) = v;
+      } else {  // (one slice)
+        v.x = a.part[at];
+        if (j + 1 < r) v.y = a.part[at + 1];
+        if (j + 2 < r) v.z = a.part[at + 2];
+        if (j + 3 < r) v.w = a.part[at + 3];
+      }
+    }
+    *reinterpret_cast<float4*>(s_sum + i * stride + j) = v;
   }
   __syncthreads();
-  const float scale = a.scale[tile.group];
-  const int chunks = (r + 31) / 32;
-  for (int o = tid; o < MT * chunks * 64; o += kShrinkThreads) {  // lane (row, 8 columns)
-    const int l = o & 63, c = (o >> 6) % chunks, t = (o >> 6) / chunks;
-    float v[8];
-    load8(sum + (16 * t + (l & 15)) * kSumStride + 32 * c + 8 * (l >> 4), v);
+  const float scale = a.scale != nullptr ? a.scale[t.group] : 1.f;
+  if (a.packed != nullptr)
+    for (int o = tid; o < 2 * chunks * 64; o += kPackThreads) {  // lane (row, 8 columns)
+      const int l = o & 63, c = (o >> 6) % chunks, h = (o >> 6) / chunks;
+      float v[8];
+      load8(s_sum + (16 * h + (l & 15)) * stride + 32 * c + 8 * (l >> 4), v);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= scale;
-    u32x4* const to = a.packed + (((size_t)tile.at * MT + t) * chunks + c) * a.split * 64 + l;
-    for (int s = 0; s < a.split; ++s) to[s * 64] = take_bf16(v);
-  }
-  if (MT == 2 && a.outer != nullptr) {
+      for (int k = 0; k < 8; ++k) v[k] *= scale;
+      u32x4* const to = a.packed + ((((size_t)t.at * 4 + 2 * half + h) * chunks + c) * a.split) * 64 + l;
+      for (int s = 0; s < a.split; ++s) to[s * 64] = take_bf16(v);
+    }
+  if (a.outer != nullptr) {
     const int tiles = (r + 15) / 16;
-    for (int o = tid; o < tiles * 64; o += kShrinkThreads) {  // lane (column, 8 rows)
+    for (int o = tid; o < tiles * 64; o += kPackThreads) {  // lane (column, 8 rows)
       const int l = o & 63, m = o >> 6;
       float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = scale * sum[(8 * (l >> 4) + k) * kSumStride + 16 * m + (l & 15)];
-      u32x4* const to = a.outer + ((size_t)tile.at * tiles + m) * 3 * 64 + l;
+      for (int k = 0; k < 8; ++k) v[k] = scale * s_sum[(8 * (l >> 4) + k) * stride + 16 * m + (l & 15)];
+      u32x4* const to = a.outer + ((size_t)t.at * 2 + half) * tiles * 3 * 64 + m * 3 * 64 + l;
 #pragma unroll
       for (int s = 0; s < 3; ++s) to[s * 64] = take_bf16(v);
     }
   }
 }
 
-inline void launch_shrink(const Shrink& a, int n_tiles, int rows, hipStream_t s) {
-  const dim3 grid(n_tiles), block(kShrinkThreads);
-  if (rows == 16) {
-    if (a.r <= 16) hipLaunchKernelGGL((shrink_kernel<1, 1>), grid, block, 0, s, a);
-    else if (a.r <= 32) hipLaunchKernelGGL((shrink_kernel<1, 2>), grid, block, 0, s, a);
-    else if (a.r <= 64) hipLaunchKernelGGL((shrink_kernel<1, 4>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((shrink_kernel<1, 8>), grid, block, 0, s, a);
-  } else {
-    if (a.r <= 16) hipLaunchKernelGGL((shrink_kernel<2, 1>), grid, block, 0, s, a);
-    else if (a.r <= 32) hipLaunchKernelGGL((shrink_kernel<2, 2>), grid, block, 0, s, a);
-    else if (a.r <= 64) hipLaunchKernelGGL((shrink_kernel<2, 4>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((shrink_kernel<2, 8>), grid, block, 0, s, a);
-  }
+static __global__ __launch_bounds__(kPackThreads) void pack_kernel(Pack a) {
+  __shared__ __align__(16) PackBuffer s_sum;
+  pack_block(a, blockIdx.x, &s_sum[0][0], kPackStride);
 }
 
-// ---- packing a P that is there already ----------------------------------------------------------------------------------------
-struct Pack {
-  const Tile* tiles;    // of 32 rows; nullptr: all rows one group
-  const int32_t* list;
-  int T;
-  const float* p;       // [T][r]
-  int r;
-  u32x4* packed;        // as Shrink's, in two parts; or nullptr
-  u32x4* outer;
-};
-__device__ __forceinline__ void pack_block(const Pack& a, int b) {
-  Tile t{0, b * 32, 0, b};
-  if (a.tiles != nullptr) t = a.tiles[b];
-  else t.rows = min(32, a.T - t.first);
-  if (t.rows == 0) return;
-  const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4, r = a.r, tiles = (r + 15) / 16, chunks = (r + 31) / 32;
-  const auto value = [&](int i, int j) {
-    if (i >= t.rows || j >= r) return 0.f;
-    const int at = t.first + i;
-    return a.p[(size_t)(a.list != nullptr ? a.list[at] : at) * r + j];
-  };
-  const int waves = blockDim.x >> 6;
-  for (int m = threadIdx.x >> 6; m < tiles; m += waves) {
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = value(8 * q + i, 16 * m + c);
-    u32x4* const to = a.outer + ((size_t)t.at * tiles + m) * 3 * 64 + lane;
-#pragma unroll
-    for (int s = 0; s < 3; ++s) to[s * 64] = take_bf16(v);
-  }
-  if (a.packed == nullptr) return;
-  for (int o = threadIdx.x >> 6; o < 2 * chunks; o += waves) {
-    const int h = o & 1, k = o >> 1;
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = value(16 * h + c, 32 * k + 8 * q + i);
-    u32x4* const to = a.packed + (((size_t)t.at * 2 + h) * chunks + k) * 2 * 64 + lane;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) to[s * 64] = take_bf16(v);
-  }
-}
-
-// Bytes of both forms for n tiles of 16 and of 32 rows.
-inline size_t packed_bytes(int n, int r, int split) { return (size_t)n * ceil_div(r, 32) * split * 1024; }
-inline size_t outer_bytes(int n, int r) { return (size_t)n * ceil_div(r, 16) * 3 * 1024; }
+// Bytes of both forms for n tiles.
+inline size_t packed_bytes(int n, int r, int split) { return (size_t)n * 4 * ceil_div(r, 32) * split * 1024; }
+inline size_t outer_bytes(int n, int r) { return (size_t)n * 2 * ceil_div(r, 16) * 3 * 1024; }
 
 // ---- expand ------------------------------------------------------------------------------------------------------------------
 // A wavefront computes up to 64 rows of 16 NJ columns, 16 rows at a time.  The MFMA's first operand is P, its second M_a; accumulator j of
@@ -448,18 +455,17 @@ struct Expand {
   int m_stride, N;
   const void* y_in;     // [T][N] or nullptr
   void* y_out;          // [T][N]
-  float* keep;          // zeroed for rows without a group, or nullptr
 };
 
-// `n` rows without a group: the output is the input, `keep` is 0.
+// `n` rows without a group: the output is the input.
 template <typename YT>
-__device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, float* keep, int r, int N, const int32_t* s_rows, int n, int c0,
-                                          int cols) {
+__device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, int N, const int32_t* s_rows, int n, int c0, int cols) {
   constexpr int W = 16 / sizeof(YT);
   const YT* in = static_cast<const YT*>(y_in);
   YT* out = static_cast<YT*>(y_out);
   cols = min(cols, N - c0);
-  if (in != out) {
+  if (in == out) return;
+  {
     const int per_row = cols / W, total = n * per_row;
     for (int i0 = threadIdx.x; i0 < total; i0 += 8 * kExpandThreads) {
       u32x4 v[8];
@@ -475,29 +481,27 @@ __device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, float* 
         if (i0 + u * kExpandThreads < total) *reinterpret_cast<u32x4*>(out + at[u]) = v[u];
     }
   }
-  if (keep != nullptr && c0 == 0)
-    for (int i = threadIdx.x; i < n * r; i += kExpandThreads) keep[(size_t)s_rows[i / r] * r + i % r] = 0.f;
 }
 
 template <typename YT, int SPLIT, int PARTS, int CH, int NJ>
 __global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e) {
   constexpr int BYTES = NJ * (int)sizeof(YT) < 16 ? NJ * (int)sizeof(YT) : 16, W = BYTES / (int)sizeof(YT), UNITS = NJ / W;
-  constexpr int COLS = 16 * NJ, U = kExpandRows / 16;
+  constexpr int COLS = 16 * NJ, U = kTileRows / 16;
   typedef uint32_t unit __attribute__((ext_vector_type(BYTES / 4)));
-  __shared__ int32_t s_rows[kExpandRows];
+  __shared__ int32_t s_rows[kTileRows];
   __shared__ __align__(16) char s_buf[kExpandWaves * COLS * 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, q = lane >> 4;
-  Tile tile{0, (int)blockIdx.y * kExpandRows, 0, (int)blockIdx.y * U};
+  Tile tile{0, (int)blockIdx.y * kTileRows, 0, (int)blockIdx.y};
   if (e.tiles != nullptr) tile = e.tiles[blockIdx.y];
-  else tile.rows = min(kExpandRows, e.T - tile.first);
+  else tile.rows = min(kTileRows, e.T - tile.first);
   if (tile.rows == 0) return;
-  if (tid < kExpandRows) {
+  if (tid < kTileRows) {
     const int at = tile.first + min(tid, tile.rows - 1);
     s_rows[tid] = e.list != nullptr ? e.list[at] : at;
   }
   __syncthreads();
   if (tile.group == e.L) {
-    copy_rows<YT>(e.y_in, e.y_out, e.keep, e.r, e.N, s_rows, tile.rows, blockIdx.x * kExpandWaves * COLS, kExpandWaves * COLS);
+    copy_rows<YT>(e.y_in, e.y_out, e.N, s_rows, tile.rows, blockIdx.x * kExpandWaves * COLS, kExpandWaves * COLS);
     return;
   }
   const int nbase = (blockIdx.x * kExpandWaves + wave) * COLS;
@@ -513,7 +517,7 @@ __global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e) {
   const int in_last = in != nullptr ? e.N - W : 0;
   const size_t in_stride = in != nullptr ? e.N : 0;
   const auto load = [&](unit(&yy)[4][UNITS], u32x4(&pp)[CH][SPLIT], int u) {
-    const u32x4* const from = e.packed + ((size_t)tile.at + u) * chunks * SPLIT * 64 + lane;
+    const u32x4* const from = e.packed + ((size_t)tile.at * U + u) * chunks * SPLIT * 64 + lane;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -655,7 +659,8 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
   const int blocks = (tile.rows + 31) / 32;
   const u32x4* const packed = sd.packed + ((size_t)tile.at * tiles + m0) * 3 * 64 + lane;
   const int m_last = min(MT, tiles - m0) - 1;  // (tiles past the last: computed from it again and not stored)
-  u32x4 z[8];
+  constexpr int FIRST = MT < 2 ? MT : 2;  // tiles of P's columns whose parts are loaded a block ahead
+  u32x4 z[8], p[FIRST][3];
   const auto load_z = [&](int b) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -663,38 +668,50 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
       z[i] = *reinterpret_cast<const u32x4*>(zc + (size_t)(o.list != nullptr ? s_rows[at] : tile.first + at) * sd.cols);
     }
   };
+  const auto load_p = [&](u32x4(&v)[3], int b, int m) {
+#pragma unroll
+    for (int s = 0; s < 3; ++s) v[s] = packed[((size_t)b * tiles + min(m, m_last)) * 3 * 64 + s * 64];
+  };
   int b = wave;
-  if (b < blocks) load_z(b);
+  if (b < blocks) {
+#pragma unroll
+    for (int m = 0; m < FIRST; ++m) load_p(p[m], b, m);
+    load_z(b);
+  }
   for (; b < blocks; b += kOuterWaves) {
-    u32x4 f[8];
+    const int next = min(b + kOuterWaves, blocks - 1);
+    u32x4 f[8], late[MT > FIRST ? MT - FIRST : 1][3];
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
       uint32_t lo[4], hi[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t x = z[2 * i][d], y = z[2 * i + 1][d];
-        lo[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-        hi[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        lo[i] = __builtin_amdgcn_perm(z[2 * i + 1][d], z[2 * i][d], 0x05040100u);
+        hi[i] = __builtin_amdgcn_perm(z[2 * i + 1][d], z[2 * i][d], 0x07060302u);
       }
       f[2 * d] = u32x4{lo[0], lo[1], lo[2], lo[3]};
       f[2 * d + 1] = u32x4{hi[0], hi[1], hi[2], hi[3]};
     }
-    const u32x4* const from = packed + (size_t)b * tiles * 3 * 64;
-    u32x4 p[2][3];
+    // loads return in the order they are issued in: P's for this block, P's for the next, Z's for the next
 #pragma unroll
-    for (int s = 0; s < 3; ++s) p[0][s] = from[s * 64];
+    for (int m = FIRST; m < MT; ++m) load_p(late[m - FIRST], b, m);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      if (m + 1 < MT)
-#pragma unroll
-        for (int s = 0; s < 3; ++s) p[(m + 1) & 1][s] = from[min(m + 1, m_last) * 3 * 64 + s * 64];
-      else  // Z's next rows behind the last of P: loads return in order
-        load_z(min(b + kOuterWaves, blocks - 1));
+    for (int m = 0; m < FIRST; ++m)
 #pragma unroll
       for (int s = 0; s < 3; ++s)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[m][j] = mfma(p[m & 1][s], f[j], acc[m][j]);
-    }
+        for (int j = 0; j < 8; ++j) acc[m][j] = mfma(p[m][s], f[j], acc[m][j]);
+#pragma unroll
+    for (int m = 0; m < FIRST; ++m) load_p(p[m], next, m);
+    load_z(next);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int m = FIRST; m < MT; ++m)
+#pragma unroll
+      for (int s = 0; s < 3; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[m][j] = mfma(late[m - FIRST][s], f[j], acc[m][j]);
   }
   const int slot = o.pieces != nullptr ? o.slots[blockIdx.y] : (o.T > o.chunk ? (int)blockIdx.y : -1);
   const float scale = sd.scale != nullptr ? sd.scale[tile.group] : 1.f;
