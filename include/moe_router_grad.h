@@ -31,7 +31,7 @@ extern "C" {
  *   losses[0]    = E / (k Tv) * sum_e counts[e] * mean_prob[e]         (1 when both are even)
  *   losses[1]    = mean over the counting tokens of (log sum_e exp logits[t,e])^2
  * With Tv == 0 all of them are 0.
- * logits     [T,E] fp32; -inf excludes an expert for a token, which needs one finite logit; a row that does not count is not read
+ * logits     [T,E] fp32; -inf excludes an expert for a token, which needs one finite logit; a row that does not count may hold anything
  * topk_idx   [T,k] int32; ids outside [0,E) are not counted
  * token_mask [T] bytes, or NULL
  * counts     [E+1] int32, mean_prob [E] fp32, losses [2] fp32
@@ -55,7 +55,7 @@ size_t moe_balance_workspace_bytes(int32_t T, int32_t E);
  * coef_*     finite
  * flags      0 or MOE_RENORM_TOPK, as in the forward call
  * d_logits   [T,E] fp32, written whole
- * With d_topk_w == NULL a row that does not count is not read (its gradient is 0).  Sizes as above.
+ * With d_topk_w == NULL a row that does not count may hold anything (its gradient is 0).  Sizes as above.
  */
 int moe_route_backward(const float* logits, const int32_t* topk_idx, const float* d_topk_w, const uint8_t* token_mask,
                        const int32_t* counts, int32_t T, int32_t E, int32_t k, float coef_balance, float coef_z, uint32_t flags,

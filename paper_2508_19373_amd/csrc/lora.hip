@@ -314,10 +314,10 @@ T* at(char* ws, size_t offset) {
   return reinterpret_cast<T*>(ws + offset);
 }
 
-void launch_sort(const Plan& p, const int32_t* idx, int T, int L, char* ws, hipStream_t s) {
-  const Sort sort{idx, T, L, p.chunk, p.n_tiles, p.n_pieces, at<int32_t>(ws, p.offsets), at<int32_t>(ws, p.list),
-                  at<Tile>(ws, p.tiles), at<Tile>(ws, p.pieces), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0)};
-  hipLaunchKernelGGL(sort_kernel, dim3(1), dim3(kSortThreads), 0, s, sort);
+void sort_rows(const Plan& p, const int32_t* idx, int T, int L, char* ws, hipStream_t s) {
+  launch_sort(Sort{idx, T, L, p.chunk, p.n_tiles, p.n_pieces, at<int32_t>(ws, p.offsets), at<int32_t>(ws, p.list), at<Tile>(ws, p.tiles),
+                   at<Tile>(ws, p.pieces), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0)},
+              s);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -366,7 +366,7 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
     if (f32) launch_expand_few<float, 3>(e, s);
     else launch_expand_few<uint16_t, 2>(e, s);
   } else {
-    launch_sort(p, adapter_idx, T, n_adapters, ws, s);
+    sort_rows(p, adapter_idx, T, n_adapters, ws, s);
     const int32_t* list = at<int32_t>(ws, p.list);
     const Tile* tiles = at<Tile>(ws, p.tiles);
     float* const part = at<float>(ws, p.part);
@@ -401,7 +401,7 @@ int moe_lora_backward(const void* x_bf16, const void* dy_bf16, const int32_t* ad
   const uint16_t *x = static_cast<const uint16_t*>(x_bf16), *dy = static_cast<const uint16_t*>(dy_bf16);
   const Plan p = make_plan(T, K, N, rank, n_adapters, true);
   char* const ws = static_cast<char*>(workspace);
-  launch_sort(p, adapter_idx, T, n_adapters, ws, s);
+  sort_rows(p, adapter_idx, T, n_adapters, ws, s);
   const int32_t *list = at<int32_t>(ws, p.list), *offsets = at<int32_t>(ws, p.offsets);
   const Tile* tiles = at<Tile>(ws, p.tiles);
   u32x4 *const outer_u = at<u32x4>(ws, p.outer_u), *const outer_v = at<u32x4>(ws, p.outer_v);

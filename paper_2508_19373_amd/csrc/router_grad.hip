@@ -15,37 +15,87 @@ constexpr int kWaves = kThreads / kWave;
 
 // ---- softmax rows ----------------------------------------------------------------------------------------------------------
 // G lanes (8 to 64) share a token and its E experts, expert l + G s in slot s of the group's lane l: with 8 experts a wavefront holds
-// eight tokens, with 60 one, and every load is of neighbouring words.
-template <int G, typename Op>
-__device__ __forceinline__ float group_reduce(float v, Op op) {
-  if constexpr (G == 64) return wave_reduce(v, op);
+// eight tokens, with 60 one, and every load is of neighbouring words.  U tokens one after the other: their loads are in flight
+// together, and with 64 lanes a token four tokens' reductions are one.
+//
+// op over the group's lanes for each of U values; every lane gets them.
+template <int G, int U, typename Op>
+__device__ __forceinline__ void group_reduce(float (&v)[U], Op op) {
+#ifdef __HIP_DEVICE_COMPILE__
+  if constexpr (G == 64 && U == 4) {
+    // halves of two values side by side, quarters of four; then within 16 lanes all four at a time (row_ror:8, :4, quad_perm)
+    const auto pair = [&](float a, float b) {
+      const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+      return op(__uint_as_float(h[0]), __uint_as_float(h[1]));
+    };
+    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(pair(v[0], v[1])), __float_as_uint(pair(v[2], v[3])), false, false);
+    float x = op(__uint_as_float(q[0]), __uint_as_float(q[1]));
+    const auto move = [](float y, auto ctrl) {
+      return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    x = op(x, move(x, std::integral_constant<int, 0x128>{}));
+    x = op(x, move(x, std::integral_constant<int, 0x124>{}));
+    x = op(x, move(x, std::integral_constant<int, 0x4E>{}));
+    x = op(x, move(x, std::integral_constant<int, 0xB1>{}));
+    const int lane_of[4] = {0, 32, 16, 48};
 #pragma unroll
-  for (int d = G / 2; d >= 1; d /= 2) v = op(v, __shfl_xor(v, d));
-  return v;
+    for (int u = 0; u < 4; ++u) v[u] = __int_as_float((int)__builtin_amdgcn_readlane(__float_as_int(x), lane_of[u]));
+    return;
+  }
+#endif
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if constexpr (G == 64) {
+      v[u] = wave_reduce(v[u], op);
+    } else {
+#pragma unroll
+      for (int d = G / 2; d >= 1; d /= 2) v[u] = op(v[u], __shfl_xor(v[u], d));
+    }
+  }
 }
-template <int G>
-__device__ __forceinline__ float group_sum(float v) {
-  return group_reduce<G>(v, [](float a, float b) { return a + b; });
+template <int G, int U>
+__device__ __forceinline__ void group_sum(float (&v)[U]) {
+  group_reduce<G, U>(v, [](float a, float b) { return a + b; });
 }
 
-// p: the token's logits on entry (-inf past E), its softmax on return; returns log sum exp.
-template <int G, int S>
-__device__ __forceinline__ float group_softmax(float (&p)[S]) {
-  float top = p[0];
+// 1 / v to the last place or so: the hardware's estimate and one step.
+__device__ __forceinline__ float reciprocal(float v) {
+#ifdef __HIP_DEVICE_COMPILE__
+  const float r = __builtin_amdgcn_rcpf(v);
+  return fmaf(fmaf(-v, r, 1.f), r, r);
+#else
+  return 1.f / v;
+#endif
+}
+
+// p: the tokens' logits on entry, their softmax on return (0 past E); lse: log sum exp.
+template <int G, int S, int U>
+__device__ __forceinline__ void group_softmax(float (&p)[U][S], int l, int E, float (&lse)[U]) {
+  float top[U], sum[U];
 #pragma unroll
-  for (int s = 1; s < S; ++s) top = fmaxf(top, p[s]);
-  top = group_reduce<G>(top, [](float a, float b) { return fmaxf(a, b); });
-  float sum = 0.f;
+  for (int u = 0; u < U; ++u) {
+    top[u] = -INFINITY;
 #pragma unroll
-  for (int s = 0; s < S; ++s) {
-    p[s] = expf(p[s] - top);
-    sum += p[s];
+    for (int s = 0; s < S; ++s) top[u] = fmaxf(top[u], l + G * s < E ? p[u][s] : -INFINITY);
   }
-  sum = group_sum<G>(sum);
-  const float inv = 1.f / sum;
+  group_reduce<G, U>(top, [](float a, float b) { return fmaxf(a, b); });
 #pragma unroll
-  for (int s = 0; s < S; ++s) p[s] *= inv;
-  return top + logf(sum);
+  for (int u = 0; u < U; ++u) {
+    sum[u] = 0.f;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      p[u][s] = l + G * s < E ? expf(p[u][s] - top[u]) : 0.f;
+      sum[u] += p[u][s];
+    }
+  }
+  group_sum<G, U>(sum);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const float inv = reciprocal(sum[u]);
+#pragma unroll
+    for (int s = 0; s < S; ++s) p[u][s] *= inv;
+    lse[u] = top[u] + logf(sum[u]);
+  }
 }
 
 // ---- balance loss ----------------------------------------------------------------------------------------------------------
@@ -93,7 +143,7 @@ __device__ __forceinline__ void balance_finish(const Balance& b, const int32_t* 
 
 template <int G, int S>
 __global__ __launch_bounds__(kLossThreads) void balance_kernel(Balance b) {
-  constexpr int kGroups = kLossThreads / G;
+  constexpr int kGroups = kLossThreads / G, U = G == 64 ? 4 : 2, PICKED = G < MOE_MAX_TOPK ? 2 : 1;
   __shared__ int32_t cnt[MOE_MAX_EXPERTS + 1];
   __shared__ float sums[kGroups][G * S], zsum[kGroups], total[MOE_MAX_EXPERTS + 1], red[kLossWaves];
   const int tid = threadIdx.x, l = tid & (G - 1), group = tid / G, E = b.E;
@@ -102,21 +152,34 @@ __global__ __launch_bounds__(kLossThreads) void balance_kernel(Balance b) {
   float mine[S], z = 0.f;
 #pragma unroll
   for (int s = 0; s < S; ++s) mine[s] = 0.f;
+  // (no load under a condition, which would be waited for at once)
+  const uint8_t* const mask = b.mask != nullptr ? b.mask : reinterpret_cast<const uint8_t*>(b.logits);
   const int step = gridDim.x * kGroups;
-  for (int t = blockIdx.x * kGroups + group; t < b.T; t += step) {
-    if (b.mask != nullptr && b.mask[t] == 0) continue;
-    float p[S];
+  for (int t0 = blockIdx.x * kGroups + group; t0 < b.T; t0 += U * step) {
+    float p[U][S], lse[U];
+    int e[U][PICKED];
+    bool in[U];
 #pragma unroll
-    for (int s = 0; s < S; ++s) p[s] = l + G * s < E ? b.logits[(size_t)t * E + l + G * s] : -INFINITY;
-    for (int j = l; j < b.k; j += G) {
-      const int e = b.idx[(size_t)t * b.k + j];
-      if ((unsigned)e < (unsigned)E) atomicAdd(&cnt[e], 1);
+    for (int u = 0; u < U; ++u) {
+      const int t = min(t0 + u * step, b.T - 1);
+      in[u] = mask[b.mask != nullptr ? t : 0] != 0 || b.mask == nullptr;
+#pragma unroll
+      for (int s = 0; s < S; ++s) p[u][s] = b.logits[(size_t)t * E + min(l + G * s, E - 1)];
+#pragma unroll
+      for (int i = 0; i < PICKED; ++i) e[u][i] = b.idx[(size_t)t * b.k + min(l + G * i, b.k - 1)];
     }
-    if (l == 0) atomicAdd(&cnt[E], 1);
-    const float lse = group_softmax<G, S>(p);
-    z = fmaf(lse, lse, z);
+    group_softmax<G, S, U>(p, l, E, lse);
 #pragma unroll
-    for (int s = 0; s < S; ++s) mine[s] += p[s];
+    for (int u = 0; u < U; ++u) {
+      if (!in[u] || t0 + u * step >= b.T) continue;
+#pragma unroll
+      for (int i = 0; i < PICKED; ++i)
+        if (l + G * i < b.k && (unsigned)e[u][i] < (unsigned)E) atomicAdd(&cnt[e[u][i]], 1);
+      if (l == 0) atomicAdd(&cnt[E], 1);
+      z = fmaf(lse[u], lse[u], z);
+#pragma unroll
+      for (int s = 0; s < S; ++s) mine[s] += p[u][s];
+    }
   }
 #pragma unroll
   for (int s = 0; s < S; ++s) sums[group][l + G * s] = mine[s];
@@ -124,6 +187,7 @@ __global__ __launch_bounds__(kLossThreads) void balance_kernel(Balance b) {
   __syncthreads();
   for (int e = tid; e <= E; e += kLossThreads) {
     float sum = 0.f;
+#pragma unroll 8
     for (int g = 0; g < kGroups; ++g) sum += e < E ? sums[g][e] : zsum[g];
     total[e] = sum;
   }
@@ -135,20 +199,28 @@ __global__ __launch_bounds__(kLossThreads) void balance_kernel(Balance b) {
   }
 }
 
+// 64 columns at a time, an eighth of the parts a wavefront, sixteen of them in flight.
 __global__ __launch_bounds__(kLossThreads) void balance_join_kernel(Balance b, int parts) {
   __shared__ int32_t cnt[MOE_MAX_EXPERTS + 1], s_cnt[kLossWaves][kWave];
   __shared__ float total[MOE_MAX_EXPERTS + 1], s_sum[kLossWaves][kWave], red[kLossWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, E1 = b.E + 1;
-  for (int e0 = 0; e0 < E1; e0 += kWave) {  // 64 columns at a time, a share of the parts a wavefront
-    const int e = e0 + lane;
+  for (int e0 = 0; e0 < E1; e0 += kWave) {
+    const int e = e0 + lane, at = min(e, E1 - 1);
     float sum = 0.f;
     int c = 0;
-    if (e < E1)
-#pragma unroll 8
-      for (int p = wave; p < parts; p += kLossWaves) {
-        sum += b.part_prob[(size_t)p * E1 + e];
-        c += b.part_cnt[(size_t)p * E1 + e];
+    for (int p0 = wave; p0 < parts; p0 += 16 * kLossWaves) {
+      float v[16];
+      int n[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        const size_t from = (size_t)min(p0 + u * kLossWaves, parts - 1) * E1 + at;
+        v[u] = b.part_prob[from];
+        n[u] = b.part_cnt[from];
       }
+#pragma unroll
+      for (int u = 0; u < 16; ++u)
+        if (p0 + u * kLossWaves < parts) sum += v[u], c += n[u];
+    }
     s_sum[wave][lane] = sum;
     s_cnt[wave][lane] = c;
     __syncthreads();
@@ -176,59 +248,97 @@ struct RouteBackward {
   float* d_logits;
 };
 
-template <int G, int S>
+// The gradients at the picked experts, k values of a token, come to the lanes of these experts through LDS (a group's own piece of
+// it).  The losses' part is p (f - sum p f), that of the gates the same with their own softmax, which without renormalisation is p too:
+// one dot product serves both then.
+template <int G, int S, int U>
 __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward b) {
-  const int l = threadIdx.x & (G - 1), E = b.E, k = b.k;
-  const int t = blockIdx.x * (kThreads / G) + threadIdx.x / G;
-  if (t >= b.T) return;
-  const bool counted = b.counts != nullptr && (b.mask == nullptr || b.mask[t] != 0);
-  float d[S];
+  constexpr int PICKED = G < MOE_MAX_TOPK ? 2 : 1;  // a lane's share of a token's picked experts
+  __shared__ float2 s_picked[kThreads / G][U][G * S];  // (1 if picked, gradient)
+  const int l = threadIdx.x & (G - 1), group = threadIdx.x / G, E = b.E, k = b.k;
+  const int t0 = (blockIdx.x * (kThreads / G) + group) * U;
+  if (t0 >= b.T) return;
+  // (no load under a condition, which would be waited for at once: what is not there is read from the logits and not used)
+  const bool gates = b.d_topk_w != nullptr, losses = b.counts != nullptr;
+  const uint8_t* const mask = b.mask != nullptr ? b.mask : reinterpret_cast<const uint8_t*>(b.logits);
+  const float* const d_topk_w = gates ? b.d_topk_w : b.logits;
+  float p[U][S], lse[U], load[S], grads[U][PICKED];
+  int ids[U][PICKED];
+  bool counted[U];
 #pragma unroll
-  for (int s = 0; s < S; ++s) d[s] = 0.f;
-  if (counted || b.d_topk_w != nullptr) {
-    float p[S];
+  for (int u = 0; u < U; ++u) {
+    const size_t t = min(t0 + u, b.T - 1);
+    counted[u] = (mask[b.mask != nullptr ? t : 0] != 0 || b.mask == nullptr) && losses;
 #pragma unroll
-    for (int s = 0; s < S; ++s) p[s] = l + G * s < E ? b.logits[(size_t)t * E + l + G * s] : -INFINITY;
-    const float lse = group_softmax<G, S>(p);
-    if (b.d_topk_w != nullptr) {
-      // gates: the softmax over all experts, or over the picked ones alone; dw: the gradient at each picked expert
-      float w[S], dw[S], sum = 0.f, dot = 0.f;
+    for (int s = 0; s < S; ++s) p[u][s] = b.logits[t * E + min(l + G * s, E - 1)];
 #pragma unroll
-      for (int s = 0; s < S; ++s) w[s] = b.renorm ? 0.f : p[s], dw[s] = 0.f;
-      for (int j = 0; j < k; ++j) {
-        const int e = b.idx[(size_t)t * k + j];
-        const float g = b.d_topk_w[(size_t)t * k + j];
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-          if (e == l + G * s) w[s] = p[s], dw[s] = g;
-      }
-#pragma unroll
-      for (int s = 0; s < S; ++s) sum += w[s];
-      const float inv = b.renorm ? 1.f / group_sum<G>(sum) : 1.f;
-#pragma unroll
-      for (int s = 0; s < S; ++s) w[s] *= inv, dot = fmaf(w[s], dw[s], dot);
-      dot = group_sum<G>(dot);
-#pragma unroll
-      for (int s = 0; s < S; ++s) d[s] = w[s] * (dw[s] - dot);
-    }
-    if (counted) {
-      // the load's gradient is the same with a constant taken off: off the even load, which leaves small numbers to subtract
-      const float many = fmaxf((float)b.counts[E], 1.f), even = (float)k * many / (float)E;
-      const float c = b.coef_balance * (float)E / ((float)k * many * many), cz = 2.f * b.coef_z / many * lse;
-      float g[S], dot = 0.f;
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        g[s] = l + G * s < E ? c * ((float)b.counts[l + G * s] - even) : 0.f;
-        dot = fmaf(p[s], g[s], dot);
-      }
-      dot = group_sum<G>(dot);
-#pragma unroll
-      for (int s = 0; s < S; ++s) d[s] += p[s] * (g[s] - dot + cz);
+    for (int i = 0; i < PICKED; ++i) {
+      ids[u][i] = b.idx[t * k + min(l + G * i, k - 1)];
+      grads[u][i] = d_topk_w[gates ? t * k + min(l + G * i, k - 1) : 0];
     }
   }
+  // the load's gradient is the same with a constant taken off: off the even load, which leaves small numbers to subtract
+  float cz = 0.f;
 #pragma unroll
-  for (int s = 0; s < S; ++s)
-    if (l + G * s < E) b.d_logits[(size_t)t * E + l + G * s] = d[s];
+  for (int s = 0; s < S; ++s) load[s] = 0.f;
+  if (losses) {
+    const float many = fmaxf((float)b.counts[E], 1.f), even = (float)k * many / (float)E;
+    const float c = b.coef_balance * (float)E / ((float)k * many * many);
+    cz = 2.f * b.coef_z / many;
+#pragma unroll
+    for (int s = 0; s < S; ++s) load[s] = l + G * s < E ? c * ((float)b.counts[l + G * s] - even) : 0.f;
+  }
+  if (gates) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int s = 0; s < S; ++s) s_picked[group][u][l + G * s] = make_float2(0.f, 0.f);
+    wave_fence();
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < PICKED; ++i)
+        if (l + G * i < k && (unsigned)ids[u][i] < (unsigned)E) s_picked[group][u][ids[u][i]] = make_float2(1.f, grads[u][i]);
+    wave_fence();
+  }
+  group_softmax<G, S, U>(p, l, E, lse);
+  float f[U][S], gate_dot[U], gate_sum[U], dot[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    gate_dot[u] = gate_sum[u] = dot[u] = 0.f;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const float2 v = gates ? s_picked[group][u][l + G * s] : make_float2(0.f, 0.f);
+      f[u][s] = counted[u] ? load[s] : 0.f;
+      if (b.renorm) {
+        gate_sum[u] = fmaf(v.x, p[u][s], gate_sum[u]);
+        gate_dot[u] = fmaf(v.y, p[u][s], gate_dot[u]);
+      } else {
+        f[u][s] += v.y;
+      }
+      dot[u] = fmaf(p[u][s], f[u][s], dot[u]);
+    }
+  }
+  group_sum<G, U>(dot);
+  if (b.renorm && gates) {
+    group_sum<G, U>(gate_sum);
+    group_sum<G, U>(gate_dot);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (t0 + u >= b.T) break;
+    const float z = counted[u] ? cz * lse[u] : 0.f;
+    const float inv = b.renorm && gates ? reciprocal(gate_sum[u]) : 0.f, mean = gate_dot[u] * inv;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      float d = counted[u] || (gates && !b.renorm) ? p[u][s] * (f[u][s] - dot[u] + z) : 0.f;
+      if (b.renorm && gates) {
+        const float2 v = s_picked[group][u][l + G * s];
+        if (v.x != 0.f) d = fmaf(p[u][s] * inv, v.y - mean, d);
+      }
+      if (l + G * s < E) b.d_logits[(size_t)(t0 + u) * E + l + G * s] = d;
+    }
+  }
 }
 
 // One kernel for each number of lanes a token needs.
@@ -242,11 +352,11 @@ void by_width(int E, Args... args) {
   else Launch<64, 4>::run(args...);
 }
 
-// About 64 tokens a wavefront's worth of work, at most two workgroups a compute unit.
+// Two steps of two tokens for each group of lanes, at most a workgroup a compute unit (one kernel more joins them).
 int loss_workgroups(int T, int E) {
   const int lanes = E <= 8 ? 8 : (E <= 16 ? 16 : (E <= 32 ? 32 : 64));
   const int n = ceil_div(T, 4 * (kLossThreads / lanes));
-  return n < 1 ? 1 : (n > 512 ? 512 : n);
+  return n < 1 ? 1 : (n > 256 ? 256 : n);
 }
 
 template <int G, int S>
@@ -258,7 +368,11 @@ struct LaunchBalance {
 template <int G, int S>
 struct LaunchRoute {
   static void run(const RouteBackward& b, hipStream_t s) {
-    hipLaunchKernelGGL((route_backward_kernel<G, S>), dim3(ceil_div(b.T, kThreads / G)), dim3(kThreads), 0, s, b);
+    // four tokens a group of lanes from a wavefront for each of the chip's places on
+    if ((int64_t)b.T * G >= (int64_t)64 * 8192)
+      hipLaunchKernelGGL((route_backward_kernel<G, S, 4>), dim3(ceil_div(b.T, 4 * (kThreads / G))), dim3(kThreads), 0, s, b);
+    else
+      hipLaunchKernelGGL((route_backward_kernel<G, S, 1>), dim3(ceil_div(b.T, kThreads / G)), dim3(kThreads), 0, s, b);
   }
 };
 

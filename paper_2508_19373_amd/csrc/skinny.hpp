@@ -26,6 +26,13 @@ __device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, f32x4 c) {
                                                  0, 0);
 }
 
+// Between LDS accesses by which lanes of one wavefront hand values to each other: the hardware keeps them in order, the compiler has to.
+__device__ __forceinline__ void wave_fence() {
+#ifdef __HIP_DEVICE_COMPILE__
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#endif
+}
+
 // The highest 8 bits of eight floats as bf16; `v` keeps the rest, which is exact.
 __device__ __forceinline__ u32x4 take_bf16(float (&v)[8]) {
   uint32_t p[4];
@@ -76,15 +83,16 @@ struct Sort {
   int32_t* slot0;            // [L] that of a group's first piece
 };
 
-// Rank of this lane among the lanes of its wavefront with the same group, and how many there are: a ballot for each bit of the id.
-__device__ __forceinline__ int match_rank(int g, bool in, int lane, int bits, int& count) {
-  unsigned long long same = __ballot(in);
+// The lanes of the wavefront with this lane's group: a ballot for each bit of the id.  Prompts lie in runs, so often it is all of them.
+__device__ __forceinline__ unsigned long long match_lanes(int g, bool in, int bits) {
+  const unsigned long long all = __ballot(in);
+  if (__ballot(in && g == (int)__builtin_amdgcn_readfirstlane(g)) == ~0ull) return all;
+  unsigned long long same = all;
   for (int b = 0; b < bits; ++b) {
     const unsigned long long set = __ballot((g >> b) & 1);
     same &= ((g >> b) & 1) ? set : ~set;
   }
-  count = __popcll(same);
-  return __popcll(same & ((1ull << lane) - 1ull));
+  return same;
 }
 
 // The last entry of pre[0 .. n] (non-decreasing) that is not above v.
@@ -98,108 +106,126 @@ __device__ __forceinline__ int find_group(const int32_t* pre, int n, int v) {
   return lo;
 }
 
-// One workgroup: each wavefront counts the groups of its share of the rows, a scan over the groups places them, the wavefronts go
-// over their rows again.  (4096 rows: four steps of 64 a wavefront, each time.  Several workgroups would need launches between the
-// steps, which cost more until there are some ten thousand rows; beyond, the products take longer by far.)
-static __global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
+// One workgroup: each wavefront counts the groups of its share of the rows, a scan over the groups places them, and the rows go to their
+// places.  ONE: up to kSortOnce rows, whose places within the share stay in registers; else the wavefronts count again.  (Several workgroups
+// would need launches between the steps, which cost more until there are some ten thousand rows; beyond, the products take longer by
+// far.)
+constexpr int kSortSteps = 8, kSortOnce = kSortWaves * kSortSteps * kWave;
+
+template <bool ONE>
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
   __shared__ int32_t cnt[kSortWaves][kMaxGroups + 1];
-  __shared__ int32_t pre[4][kMaxGroups + 2];  // prefixes over the groups of rows, tiles, pieces, slots
+  __shared__ int32_t pre[5][kMaxGroups + 2];  // prefixes over the groups of rows, tiles, whole pieces, other pieces, slots
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, groups = s.L + 1, bits = 32 - __clz(s.L);
   const int share = ((s.T + kSortWaves - 1) / kSortWaves + kWave - 1) / kWave * kWave;
   const int t0 = min(wave * share, s.T), t1 = min(t0 + share, s.T);
-  for (int g = lane; g < groups; g += kWave) cnt[wave][g] = 0;
-  const auto group_at = [&](int t) {
-    const int g = t < t1 ? s.idx[t] : 0;
-    return (unsigned)g < (unsigned)s.L ? g : s.L;
-  };
-  // 64 rows at a time; prompts lie in runs, so often all of them are one group's
-  const auto rank_of = [&](int g, bool in, int& n) {
-    if (__ballot(in && g == (int)__builtin_amdgcn_readfirstlane(g)) == ~0ull) {
-      n = kWave;
-      return lane;
+  int g[kSortSteps], place[kSortSteps];
+  const auto load_groups = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < kSortSteps; ++u) {
+      const int at = t + u * kWave + lane;
+      const int id = s.idx[min(at, s.T - 1)];
+      g[u] = (unsigned)id < (unsigned)s.L ? id : s.L;
     }
-    return match_rank(g, in, lane, bits, n);
   };
-  constexpr int B = 8;
-  for (int t = t0; t < t1; t += B * kWave) {
-    int g[B];
+  // Places of 64 rows behind each other among their group's rows that `cnt` has counted, which counts them.
+  const auto count = [&](int t) {
 #pragma unroll
-    for (int u = 0; u < B; ++u) g[u] = group_at(t + u * kWave + lane);
-#pragma unroll
-    for (int u = 0; u < B; ++u) {
+    for (int u = 0; u < kSortSteps; ++u) {
       if (t + u * kWave >= t1) break;
       const bool in = t + u * kWave + lane < t1;
-      int n;
-      const int rank = rank_of(g[u], in, n);
-      if (in && rank == 0) cnt[wave][g[u]] += n;
+      const unsigned long long same = match_lanes(g[u], in, bits);
+      const int leader = __ffsll((long long)same) - 1;
+      int before = 0;
+      if (in && lane == leader) before = atomicAdd(&cnt[wave][g[u]], (int)__popcll(same));
+      place[u] = __shfl(before, leader) + (int)__popcll(same & ((1ull << lane) - 1ull));
+    }
+  };
+  if (ONE && s.T > 0) load_groups(t0);
+  for (int e = lane; e < groups; e += kWave) cnt[wave][e] = 0;
+  wave_fence();
+  if (ONE) {
+    count(t0);
+  } else {
+    for (int t = t0; t < t1; t += kSortSteps * kWave) {
+      load_groups(t);
+      count(t);
     }
   }
   __syncthreads();
-  for (int g = tid; g < groups; g += kSortThreads) {  // rows of the group in the wavefronts before each; all of them
+  for (int e = tid; e < groups; e += kSortThreads) {  // rows of the group in the wavefronts before each; all of them
     int run = 0;
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const int c = cnt[w][g];
-      cnt[w][g] = run;
+      const int c = cnt[w][e];
+      cnt[w][e] = run;
       run += c;
     }
-    pre[0][g] = run;
+    pre[0][e] = run;
   }
   __syncthreads();
   if (wave == 0) {
-    int carry[4] = {};
-    for (int g0 = 0; g0 < groups; g0 += kWave) {
-      const int g = g0 + lane;
-      const int c = g < groups ? pre[0][g] : 0;
-      int v[4] = {c, (c + kTileRows - 1) / kTileRows, 0, 0};
-      if (s.chunk > 0 && g < s.L) {
-        v[2] = max(1, (c + s.chunk - 1) / s.chunk);
-        v[3] = c > s.chunk ? v[2] : 0;
+    int carry[5] = {};
+    for (int e0 = 0; e0 < groups; e0 += kWave) {
+      const int e = e0 + lane;
+      const int c = e < groups ? pre[0][e] : 0;
+      int v[5] = {c, (c + kTileRows - 1) / kTileRows, 0, 0, 0};
+      if (s.chunk > 0 && e < s.L) {
+        v[2] = c / s.chunk;
+        v[3] = c % s.chunk != 0 || c == 0;
+        v[4] = c > s.chunk ? v[2] + v[3] : 0;
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < 5; ++k) {
         const int incl = gg::wave_incl_scan(v[k]);
-        if (g < groups) pre[k][g] = carry[k] + incl - v[k];
+        if (e < groups) pre[k][e] = carry[k] + incl - v[k];
         carry[k] += (int)__builtin_amdgcn_readlane(incl, kWave - 1);
       }
     }
     if (lane == 0)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) pre[k][groups] = carry[k];
+      for (int k = 0; k < 5; ++k) pre[k][groups] = carry[k];
   }
   __syncthreads();
-  for (int g = tid; g <= groups; g += kSortThreads) s.offsets[g] = pre[0][g];
-  for (int t = t0; t < t1; t += B * kWave) {
-    int g[B];
+  for (int e = tid; e <= groups; e += kSortThreads) s.offsets[e] = pre[0][e];
+  for (int t = t0; t < t1; t += kSortSteps * kWave) {
+    if (!ONE) {
+      load_groups(t);
+      count(t);  // (`cnt` goes on from the rows before)
+    }
 #pragma unroll
-    for (int u = 0; u < B; ++u) g[u] = group_at(t + u * kWave + lane);
-#pragma unroll
-    for (int u = 0; u < B; ++u) {
-      if (t + u * kWave >= t1) break;
+    for (int u = 0; u < kSortSteps; ++u) {
       const int row = t + u * kWave + lane;
-      const bool in = row < t1;
-      int n;
-      const int rank = rank_of(g[u], in, n);
-      if (in) s.list[pre[0][g[u]] + cnt[wave][g[u]] + rank] = row;
-      if (in && rank == 0) cnt[wave][g[u]] += n;
+      if (row < t1) s.list[pre[0][g[u]] + place[u] + (ONE ? cnt[wave][g[u]] : 0)] = row;
     }
   }
-  for (int i = tid; i < s.n_tiles + s.n_pieces; i += kSortThreads) {
-    const bool tile = i < s.n_tiles;
-    const int b = tile ? i : i - s.n_tiles, kind = tile ? 1 : 2, rows = tile ? kTileRows : s.chunk;
+  for (int i = tid; i < s.n_tiles; i += kSortThreads) {
+    Tile t{-1, 0, 0, 0};
+    if (i < pre[1][groups]) {
+      const int e = find_group(pre[1], groups, i), k = (i - pre[1][e]) * kTileRows, n = pre[0][e + 1] - pre[0][e];
+      t = Tile{e, pre[0][e] + k, min(kTileRows, n - k), i};
+    }
+    s.tiles[i] = t;
+  }
+  const int whole = pre[2][groups];
+  for (int i = tid; i < s.n_pieces; i += kSortThreads) {  // the whole pieces first: workgroups that end last are short ones
     Tile t{-1, 0, 0, 0};
     int slot = -1;
-    if (b < pre[kind][groups]) {
-      const int g = find_group(pre[kind], groups, b), p = b - pre[kind][g], n = pre[0][g + 1] - pre[0][g];
-      t = Tile{g, pre[0][g] + p * rows, min(rows, n - p * rows), tile ? b : pre[1][g] * (kTileRows / 32) + p * rows / 32};
-      if (!tile) {
-        if (n > s.chunk) slot = pre[3][g] + p;
-        if (p == 0) s.slot0[g] = slot;
-      }
+    if (i < whole + pre[3][groups]) {
+      const int e = i < whole ? find_group(pre[2], groups, i) : find_group(pre[3], groups, i - whole);
+      const int n = pre[0][e + 1] - pre[0][e], p = i < whole ? i - pre[2][e] : n / s.chunk, k = p * s.chunk;
+      t = Tile{e, pre[0][e] + k, min(s.chunk, n - k), pre[1][e] * (kTileRows / 32) + k / 32};
+      if (n > s.chunk) slot = pre[4][e] + p;
+      if (p == 0) s.slot0[e] = slot;
     }
-    if (tile) s.tiles[b] = t;
-    else s.pieces[b] = t, s.slots[b] = slot;
+    s.pieces[i] = t;
+    s.slots[i] = slot;
   }
+}
+
+inline void launch_sort(const Sort& a, hipStream_t s) {
+  if (a.T <= kSortOnce) hipLaunchKernelGGL(sort_kernel<true>, dim3(1), dim3(kSortThreads), 0, s, a);
+  else hipLaunchKernelGGL(sort_kernel<false>, dim3(1), dim3(kSortThreads), 0, s, a);
 }
 
 // ---- shrink ------------------------------------------------------------------------------------------------------------------
@@ -274,6 +300,7 @@ __global__ __launch_bounds__(kShrinkThreads, 2) void shrink_kernel(Shrink a) {
       const u32x4 v = xv[k];
       *reinterpret_cast<u32x4*>(s_x + put + 1024 * k) = u32x4{in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u};
     }
+    wave_fence();
     u32x4 f[MT][2];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -284,6 +311,7 @@ __global__ __launch_bounds__(kShrinkThreads, 2) void shrink_kernel(Shrink a) {
     for (int g = 0; g < GROUPS; ++g) {
 #pragma unroll
       for (int k = 0; k < 2 * NG; ++k) *reinterpret_cast<u32x4*>(s_m + put + 1024 * k) = mv[k];
+      wave_fence();
       if (g + 1 < GROUPS) load_m(i, g + 1);
       else {
         load_m(i + 1, 0);
@@ -298,6 +326,7 @@ __global__ __launch_bounds__(kShrinkThreads, 2) void shrink_kernel(Shrink a) {
 #pragma unroll
           for (int t = 0; t < MT; ++t) acc[t][g * NG + j] = mfma(f[t][h], b, acc[t][g * NG + j]);
         }
+      wave_fence();
     }
   }
   float* const red = reinterpret_cast<float*>(s_buf);  // [wave][kRound][kRedStride]
@@ -559,9 +588,11 @@ __global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e) {
         *reinterpret_cast<u32x4*>(s_m + (j * 16 + l) * 64 + (((lane & 3) ^ (l >> 1 & 3)) * 16)) =
             u32x4{zero ? 0u : v.x, zero ? 0u : v.y, zero ? 0u : v.z, zero ? 0u : v.w};
       }
+      wave_fence();
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
         w[pt][c][j] = *reinterpret_cast<const u32x4*>(s_m + (j * 16 + ln) * 64 + ((q ^ (ln >> 1 & 3)) * 16));
+      wave_fence();
     }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
