@@ -27,6 +27,7 @@ extern "C" {
 
 #define MOE_LORA_MAX_ADAPTERS 256
 #define MOE_LORA_MAX_RANK 128
+#define MOE_LORA_MAX_COLUMNS 262144
 
 /*
  * v[t,:] = x[t,:] A_a^T (fp32, a = adapter_idx[t]),  y_out[t,:] = y_in[t,:] + scale[a] * v[t,:] B_a^T
@@ -41,7 +42,7 @@ extern "C" {
  * workspace    at least moe_lora_workspace_bytes(..., 0) bytes
  * flags        0 or MOE_OUT_F32
  * Requires T >= 0, T < 2^24, 1 <= n_adapters <= MOE_LORA_MAX_ADAPTERS, rank % 8 == 0, 8 <= rank <= MOE_LORA_MAX_RANK,
- * K % 8 == 0, N % 8 == 0, K, N >= 8.  Apart from y_in and y_out no two buffers may overlap.
+ * K % 8 == 0, N % 8 == 0, 8 <= K, N <= MOE_LORA_MAX_COLUMNS.  Apart from y_in and y_out no two buffers may overlap.
  */
 int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, int32_t K, int32_t N, int32_t rank,
                      int32_t n_adapters, const void* lora_a, const void* lora_b, const float* scale, const void* y_in,

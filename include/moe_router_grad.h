@@ -19,6 +19,8 @@
 
 #include "moe_shard.h"
 
+#define MOE_ROUTER_GRAD_MAX_HIDDEN 262144
+
 #ifdef __cplusplus
 extern "C" {
 #endif
@@ -70,7 +72,7 @@ int moe_route_backward(const float* logits, const int32_t* topk_idx, const float
  * d_w_router [H,E] fp32, written whole
  * workspace  at least moe_router_backward_workspace_bytes(T, H, E) bytes
  * The shared expert's gate (moe_combine's w_shared_gate) is the case E = 1 with d_logits = d_shared_gate.
- * Requires T >= 0, T < 2^24, 1 <= E <= MOE_MAX_EXPERTS, H % 8 == 0, H >= 8.
+ * Requires T >= 0, T < 2^24, 1 <= E <= MOE_MAX_EXPERTS, H % 8 == 0, 8 <= H <= MOE_ROUTER_GRAD_MAX_HIDDEN.
  */
 int moe_router_backward(const void* x_bf16, const float* w_router, const float* d_logits, int32_t T, int32_t H, int32_t E,
                         const void* dx_in, void* dx, float* d_w_router, void* workspace, size_t workspace_bytes, void* stream);
@@ -86,7 +88,7 @@ size_t moe_router_backward_workspace_bytes(int32_t T, int32_t H, int32_t E);
  * y_perm, slot_row, y_shared, x_bf16, w_shared_gate as in moe_combine; the last three and d_shared_gate: all NULL or none
  * d_topk_w      [T,k] fp32, d_shared_gate [T] fp32
  * flags         0 or MOE_Y_PERM_BF16, as in the forward call
- * Requires T >= 0, 1 <= k <= MOE_MAX_TOPK, H % 8 == 0, H >= 8.
+ * Requires T >= 0, T < 2^24, 1 <= k <= MOE_MAX_TOPK, H % 8 == 0, 8 <= H <= MOE_ROUTER_GRAD_MAX_HIDDEN.
  */
 int moe_combine_backward(const void* dy_bf16, const void* y_perm, const int32_t* slot_row, int32_t T, int32_t k, int32_t H,
                          const void* y_shared, const void* x_bf16, const float* w_shared_gate, float* d_topk_w,

@@ -40,6 +40,7 @@ ROUTER_GRAD_EXPORTS = ("moe_balance_loss", "moe_balance_workspace_bytes", "moe_r
                        "moe_router_backward_workspace_bytes", "moe_combine_backward")
 MOE_LORA_MAX_ADAPTERS = 256
 MOE_LORA_MAX_RANK = 128
+MOE_LORA_MAX_COLUMNS = 262144
 INT4_GROUP = 64
 DEBUG_UNIT_INTS = 5
 DEBUG_SLICE_INTS = 8
@@ -170,8 +171,31 @@ def _ptr(t):
 def _stream(stream):
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        # the lookup of torch's own launchers where there is one (0.2 us; making a Stream object takes 3)
+        look_up = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return torch.cuda.current_stream().cuda_stream if look_up is None else look_up(torch.cuda.current_device())
     return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _ptrs(*tensors):
+    """_ptr of each, all of them on the current device, to whose stream the launches go."""
+    out, device = [], None
+    for t in tensors:
+        if t is None or isinstance(t, int):
+            out.append(t)
+            continue
+        on = t.get_device()
+        if on != device:
+            import torch
+            if on < 0:
+                raise ValueError("device tensor required")
+            device = torch.cuda.current_device()
+            if on != device:
+                raise ValueError("tensors of the current device required")
+        if not t.is_contiguous():
+            raise ValueError("contiguous tensor required")
+        out.append(t.data_ptr())
+    return out
 
 
 def _check(fn: str, status: int):
@@ -260,18 +284,16 @@ def moe_lora_workspace_bytes(T, K, N, rank, n_adapters, backward=False) -> int:
 
 def moe_lora_forward(x, adapter_idx, T, K, N, rank, n_adapters, lora_a, lora_b, scale, y_in, y_out, v=None, workspace=None,
                      flags=0, stream=None):
-    _check("moe_lora_forward",
-           lib().moe_lora_forward(_ptr(x), _ptr(adapter_idx), T, K, N, rank, n_adapters, _ptr(lora_a), _ptr(lora_b),
-                                  _ptr(scale), _ptr(y_in), _ptr(y_out), _ptr(v), _ptr(workspace), _bytes(workspace), flags,
-                                  _stream(stream)))
+    p = _ptrs(x, adapter_idx, lora_a, lora_b, scale, y_in, y_out, v, workspace)
+    _check("moe_lora_forward", lib().moe_lora_forward(p[0], p[1], T, K, N, rank, n_adapters, *p[2:], _bytes(workspace), flags,
+                                                      _stream(stream)))
 
 
 def moe_lora_backward(x, dy, adapter_idx, T, K, N, rank, n_adapters, lora_a, lora_b, scale, v, dx_in, dx, grad_a, grad_b,
                       workspace=None, stream=None):
-    _check("moe_lora_backward",
-           lib().moe_lora_backward(_ptr(x), _ptr(dy), _ptr(adapter_idx), T, K, N, rank, n_adapters, _ptr(lora_a),
-                                   _ptr(lora_b), _ptr(scale), _ptr(v), _ptr(dx_in), _ptr(dx), _ptr(grad_a), _ptr(grad_b),
-                                   _ptr(workspace), _bytes(workspace), _stream(stream)))
+    p = _ptrs(x, dy, adapter_idx, lora_a, lora_b, scale, v, dx_in, dx, grad_a, grad_b, workspace)
+    _check("moe_lora_backward", lib().moe_lora_backward(p[0], p[1], p[2], T, K, N, rank, n_adapters, *p[3:], _bytes(workspace),
+                                                        _stream(stream)))
 
 
 def moe_balance_workspace_bytes(T, E) -> int:
@@ -279,16 +301,14 @@ def moe_balance_workspace_bytes(T, E) -> int:
 
 
 def moe_balance_loss(logits, topk_idx, token_mask, T, E, k, counts, mean_prob, losses, workspace=None, stream=None):
-    _check("moe_balance_loss",
-           lib().moe_balance_loss(_ptr(logits), _ptr(topk_idx), _ptr(token_mask), T, E, k, _ptr(counts), _ptr(mean_prob),
-                                  _ptr(losses), _ptr(workspace), _bytes(workspace), _stream(stream)))
+    p = _ptrs(logits, topk_idx, token_mask, counts, mean_prob, losses, workspace)
+    _check("moe_balance_loss", lib().moe_balance_loss(p[0], p[1], p[2], T, E, k, *p[3:], _bytes(workspace), _stream(stream)))
 
 
 def moe_route_backward(logits, topk_idx, d_topk_w, token_mask, counts, T, E, k, coef_balance, coef_z, flags, d_logits,
                        stream=None):
-    _check("moe_route_backward",
-           lib().moe_route_backward(_ptr(logits), _ptr(topk_idx), _ptr(d_topk_w), _ptr(token_mask), _ptr(counts), T, E, k,
-                                    coef_balance, coef_z, flags, _ptr(d_logits), _stream(stream)))
+    p = _ptrs(logits, topk_idx, d_topk_w, token_mask, counts, d_logits)
+    _check("moe_route_backward", lib().moe_route_backward(*p[:5], T, E, k, coef_balance, coef_z, flags, p[5], _stream(stream)))
 
 
 def moe_router_backward_workspace_bytes(T, H, E) -> int:
@@ -296,16 +316,14 @@ def moe_router_backward_workspace_bytes(T, H, E) -> int:
 
 
 def moe_router_backward(x, w_router, d_logits, T, H, E, dx_in, dx, d_w_router, workspace=None, stream=None):
-    _check("moe_router_backward",
-           lib().moe_router_backward(_ptr(x), _ptr(w_router), _ptr(d_logits), T, H, E, _ptr(dx_in), _ptr(dx),
-                                     _ptr(d_w_router), _ptr(workspace), _bytes(workspace), _stream(stream)))
+    p = _ptrs(x, w_router, d_logits, dx_in, dx, d_w_router, workspace)
+    _check("moe_router_backward", lib().moe_router_backward(*p[:3], T, H, E, *p[3:], _bytes(workspace), _stream(stream)))
 
 
 def moe_combine_backward(dy, y_perm, slot_row, T, k, H, y_shared, x, w_shared_gate, d_topk_w, d_shared_gate=None, flags=0,
                          stream=None):
-    _check("moe_combine_backward",
-           lib().moe_combine_backward(_ptr(dy), _ptr(y_perm), _ptr(slot_row), T, k, H, _ptr(y_shared), _ptr(x),
-                                      _ptr(w_shared_gate), _ptr(d_topk_w), _ptr(d_shared_gate), flags, _stream(stream)))
+    p = _ptrs(dy, y_perm, slot_row, y_shared, x, w_shared_gate, d_topk_w, d_shared_gate)
+    _check("moe_combine_backward", lib().moe_combine_backward(*p[:3], T, k, H, *p[3:], flags, _stream(stream)))
 
 
 def moe_debug_gemm_units(expert_offsets, cap_rows, n_col_blocks):

@@ -323,7 +323,7 @@ void sort_rows(const Plan& p, const int32_t* idx, int T, int L, char* ws, hipStr
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int size_status(int32_t T, int32_t K, int32_t N, int32_t rank, int32_t L) {
-  if (T < 0 || T >= (1 << 24) || K < 8 || N < 8 || rank < 1 || L < 1 || L > MOE_LORA_MAX_ADAPTERS) return MOE_ERR_INVALID_ARG;
+  if (T < 0 || T >= (1 << 24) || K < 8 || N < 8 || K > MOE_LORA_MAX_COLUMNS || N > MOE_LORA_MAX_COLUMNS || rank < 1 || L < 1 || L > MOE_LORA_MAX_ADAPTERS) return MOE_ERR_INVALID_ARG;
   if (K % 8 != 0 || N % 8 != 0 || rank % 8 != 0 || rank > MOE_LORA_MAX_RANK) return MOE_ERR_UNSUPPORTED_SHAPE;
   return MOE_OK;
 }

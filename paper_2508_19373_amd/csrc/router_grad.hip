@@ -506,7 +506,7 @@ int losses_status(int32_t T, int32_t E, int32_t k) {
 }
 
 int router_status(int32_t T, int32_t H, int32_t E) {
-  if (T < 0 || T >= (1 << 24) || E < 1 || E > MOE_MAX_EXPERTS || H < 8) return MOE_ERR_INVALID_ARG;
+  if (T < 0 || T >= (1 << 24) || E < 1 || E > MOE_MAX_EXPERTS || H < 8 || H > MOE_ROUTER_GRAD_MAX_HIDDEN) return MOE_ERR_INVALID_ARG;
   return H % 8 != 0 ? MOE_ERR_UNSUPPORTED_SHAPE : MOE_OK;
 }
 
@@ -604,7 +604,7 @@ int moe_combine_backward(const void* dy_bf16, const void* y_perm, const int32_t*
                          const void* y_shared, const void* x_bf16, const float* w_shared_gate, float* d_topk_w,
                          float* d_shared_gate, uint32_t flags, void* stream) {
   using namespace moe;
-  if (T < 0 || k < 1 || k > MOE_MAX_TOPK || H < 8) return MOE_ERR_INVALID_ARG;
+  if (T < 0 || T >= (1 << 24) || k < 1 || k > MOE_MAX_TOPK || H < 8 || H > MOE_ROUTER_GRAD_MAX_HIDDEN) return MOE_ERR_INVALID_ARG;
   if (flags & ~(uint32_t)MOE_Y_PERM_BF16) return MOE_ERR_INVALID_ARG;
   const bool gate = w_shared_gate != nullptr;
   if (T > 0) {

@@ -513,15 +513,17 @@ __device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, int N, 
 }
 
 template <typename YT, int SPLIT, int PARTS, int CH, int NJ>
-__global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e) {
+__global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e, int n_tiles) {
   constexpr int BYTES = NJ * (int)sizeof(YT) < 16 ? NJ * (int)sizeof(YT) : 16, W = BYTES / (int)sizeof(YT), UNITS = NJ / W;
   constexpr int COLS = 16 * NJ, U = kTileRows / 16;
   typedef uint32_t unit __attribute__((ext_vector_type(BYTES / 4)));
   __shared__ int32_t s_rows[kTileRows];
   __shared__ __align__(16) char s_buf[kExpandWaves * COLS * 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, q = lane >> 4;
-  Tile tile{0, (int)blockIdx.y * kTileRows, 0, (int)blockIdx.y};
-  if (e.tiles != nullptr) tile = e.tiles[blockIdx.y];
+  const int which = blockIdx.z * gridDim.y + blockIdx.y;
+  if (which >= n_tiles) return;
+  Tile tile{0, which * kTileRows, 0, which};
+  if (e.tiles != nullptr) tile = e.tiles[which];
   else tile.rows = min(kTileRows, e.T - tile.first);
   if (tile.rows == 0) return;
   if (tid < kTileRows) {
@@ -633,8 +635,10 @@ __global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e) {
 
 template <typename YT, int SPLIT, int PARTS, int CH, int NJ>
 void launch_expand_kernel(const Expand& e, int n_tiles, hipStream_t s) {
-  hipLaunchKernelGGL((expand_kernel<YT, SPLIT, PARTS, CH, NJ>), dim3(ceil_div(e.N, kExpandWaves * 16 * NJ), n_tiles),
-                     dim3(kExpandThreads), 0, s, e);
+  constexpr int kMaxY = 32768;  // (a grid's y is 16 bits)
+  hipLaunchKernelGGL((expand_kernel<YT, SPLIT, PARTS, CH, NJ>),
+                     dim3(ceil_div(e.N, kExpandWaves * 16 * NJ), n_tiles < kMaxY ? n_tiles : kMaxY, ceil_div(n_tiles, kMaxY)),
+                     dim3(kExpandThreads), 0, s, e, n_tiles);
 }
 
 // ---- outer -------------------------------------------------------------------------------------------------------------------

@@ -46,7 +46,8 @@ BACKWARD = dict(x=P, dy=P, idx=P, T=4, K=64, N=128, rank=16, L=3, a=P, b=P, scal
 def test_lora_refusals(lib, name, args):
     f = getattr(lib, name)
     invalid, shape, space = B.MOE_ERR_INVALID_ARG, B.MOE_ERR_UNSUPPORTED_SHAPE, B.MOE_ERR_WORKSPACE
-    for change in (dict(T=-1), dict(T=1 << 24), dict(K=0), dict(N=4), dict(rank=0), dict(L=0), dict(L=257)):
+    for change in (dict(T=-1), dict(T=1 << 24), dict(K=0), dict(N=4), dict(rank=0), dict(L=0), dict(L=257), dict(K=(1 << 18) + 8),
+                   dict(N=(1 << 18) + 8)):
         assert _call(f, args, **change) == invalid, change
     for change in (dict(K=60), dict(N=100), dict(rank=12), dict(rank=136)):
         assert _call(f, args, **change) == shape, change
@@ -99,8 +100,8 @@ COMBINE = dict(dy=P, y=P, slot=P, T=4, k=2, H=64, ys=P, x=P, ws=P, dw=P, dg=P, f
 def test_router_and_combine_backward_refusals(lib):
     invalid, shape = B.MOE_ERR_INVALID_ARG, B.MOE_ERR_UNSUPPORTED_SHAPE
     f = lib.moe_router_backward
-    for change in (dict(T=-1), dict(T=1 << 24), dict(H=0), dict(E=0), dict(E=257), dict(x=None), dict(dl=None), dict(dw=None),
-                   dict(w=None), dict(dx=None), dict(x=P + 8), dict(dw=P + 8), dict(dx=P + 8), dict(dx_in=P + 8)):
+    for change in (dict(T=-1), dict(T=1 << 24), dict(H=0), dict(H=(1 << 18) + 8), dict(E=0), dict(E=257), dict(x=None),
+                   dict(dl=None), dict(dw=None), dict(w=None), dict(dx=None), dict(x=P + 8), dict(dw=P + 8), dict(dx=P + 8), dict(dx_in=P + 8)):
         assert _call(f, ROUTER, **change) == invalid, change
     assert _call(f, ROUTER, H=60) == shape
     need = B.moe_router_backward_workspace_bytes(4, 64, 8)
@@ -108,7 +109,8 @@ def test_router_and_combine_backward_refusals(lib):
     for change in (dict(nbytes=need - 1), dict(ws=None), dict(ws=P + 4)):
         assert _call(f, ROUTER, **change) == B.MOE_ERR_WORKSPACE
     f = lib.moe_combine_backward
-    for change in (dict(T=-1), dict(k=0), dict(k=17), dict(H=0), dict(dy=None), dict(y=None), dict(slot=None), dict(dw=None),
+    for change in (dict(T=-1), dict(T=1 << 24), dict(k=0), dict(k=17), dict(H=0), dict(H=(1 << 18) + 8),
+                   dict(dy=None), dict(y=None), dict(slot=None), dict(dw=None),
                    dict(ys=None), dict(x=None), dict(ws=None), dict(dg=None), dict(flags=B.MOE_OUT_F32), dict(dy=P + 8),
                    dict(y=P + 8), dict(ys=P + 8), dict(x=P + 8), dict(ws=P + 8)):
         assert _call(f, COMBINE, **change) == invalid, change

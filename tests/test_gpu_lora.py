@@ -254,3 +254,23 @@ def test_offsets_beyond_32_bits():
     assert torch.allclose(out[some].float(), out_few.float(), rtol=2.0 ** -7, atol=0.05)
     assert torch.allclose(ga, ga_few, rtol=1e-4, atol=0.02) and torch.allclose(gb, gb_few, rtol=1e-4, atol=0.02)
     assert not out[T - 2].any()
+
+
+def test_more_tiles_than_a_grid_has_rows():
+    """4.4 million rows: over 65536 tiles of 64.  Values are small integers, so that every sum is exact in fp32 and bf16."""
+    T, K, N, r, L = 4_400_001, 8, 8, 8, 3
+    g = torch.Generator(device="cuda").manual_seed(5)
+    ints = lambda n, *s: torch.randint(-n, n + 1, s, generator=g, device="cuda").float()  # noqa: E731
+    x, a, b = ints(1, T, K).bfloat16(), ints(1, L, r, K).bfloat16(), ints(1, L, N, r).bfloat16()
+    scale = torch.tensor([1.0, 2.0, 0.5], device="cuda")
+    idx = torch.randint(-1, L, (T,), generator=g, device="cuda", dtype=torch.int32)
+    y, v = torch.full((T, N), 7.0, device="cuda"), torch.empty((T, r), device="cuda")
+    ws = torch.empty(B.moe_lora_workspace_bytes(T, K, N, r, L), dtype=torch.uint8, device="cuda")
+    B.moe_lora_forward(x, idx, T, K, N, r, L, a, b, scale, None, y, v, ws, B.MOE_OUT_F32)
+    ref_v, ref_y = torch.zeros_like(v), torch.zeros_like(y)
+    for e in range(L):
+        one = (idx == e)[:, None].float()
+        ve = (x.float() @ a[e].float().T) * one
+        ref_v += ve
+        ref_y += scale[e] * (ve @ b[e].float().T)
+    assert torch.equal(v, ref_v) and torch.equal(y, ref_y)

@@ -218,3 +218,17 @@ def test_chain_is_the_same_in_a_graph():
         torch.cuda.synchronize()
         for n in ("dtw", "counts", "prob", "losses", "dl", "dx", "dw"):
             assert torch.equal(eager[n], captured[n]), n
+
+
+def test_more_tiles_than_a_grid_has_rows():
+    """4.4 million tokens: over 65536 tiles of 64.  Values are small integers, so that every sum is exact."""
+    T, H, E = 4_400_001, 8, 4
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randint(-1, 2, (T, H), generator=g, device="cuda").bfloat16()
+    w = torch.randint(-2, 3, (H, E), generator=g, device="cuda").float()
+    dl = torch.randint(-1, 2, (T, E), generator=g, device="cuda").float()
+    dx, dw = torch.empty((T, H), dtype=torch.bfloat16, device="cuda"), torch.empty((H, E), device="cuda")
+    ws = torch.empty(B.moe_router_backward_workspace_bytes(T, H, E), dtype=torch.uint8, device="cuda")
+    B.moe_router_backward(x, w, dl, T, H, E, None, dx, dw, ws)
+    assert torch.equal(dx.float(), dl @ w.T)
+    assert torch.equal(dw.double(), x.double().T @ dl.double())
