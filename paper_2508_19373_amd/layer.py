@@ -80,6 +80,40 @@ def shared_on_streaming_tiles(shared_shard, T, y_perm_bf16) -> bool:
     return not y_perm_bf16 and bool(B.moe_debug_flow(T, shared_shard) & B.DEBUG_FLOW_GATEUP)
 
 
+class Adapters(NamedTuple):
+    """Low-rank adapters of many requests beside one projection: scale[i] * b[i] a[i] for adapter i."""
+    a: torch.Tensor       # [L][rank][K] bf16
+    b: torch.Tensor       # [L][N][rank] bf16
+    scale: torch.Tensor   # [L] fp32
+
+
+class Gradients(NamedTuple):
+    """What ExpertShardLayer.backward leaves: views of the layer's buffers, valid until its next call of it."""
+    dx: torch.Tensor | None              # [T,H] bf16
+    logits: torch.Tensor                 # [T,E] fp32
+    w_router: torch.Tensor | None        # [H,E] fp32
+    w_shared_gate: torch.Tensor | None   # [H] fp32
+    adapter_a: torch.Tensor | None       # [L][rank][H] fp32
+    adapter_b: torch.Tensor | None       # [L][H][rank] fp32
+
+
+def _adapters(given, K, N, pad_to=None) -> Adapters:
+    """(a, b, scale) with the checks that the kernels cannot make; a's columns padded with zeros as the weights are."""
+    a, b, scale = given
+    L, rank = a.shape[:2]
+    if tuple(a.shape) != (L, rank, K) or tuple(b.shape) != (L, N, rank) or tuple(scale.shape) != (L,):
+        raise ValueError("adapters: a [L][rank][%d], b [L][%d][rank], scale [L]" % (K, N))
+    if a.dtype != torch.bfloat16 or b.dtype != torch.bfloat16 or scale.dtype != torch.float32:
+        raise ValueError("adapters: a and b in bf16, scale in fp32")
+    if not 1 <= L <= B.MOE_LORA_MAX_ADAPTERS or rank % 8 != 0 or not 8 <= rank <= B.MOE_LORA_MAX_RANK:
+        raise ValueError("adapters: 1 to %d, ranks of 8 to %d in steps of 8" % (B.MOE_LORA_MAX_ADAPTERS, B.MOE_LORA_MAX_RANK))
+    if pad_to is not None and pad_to != K:
+        whole = torch.zeros((L, rank, pad_to), dtype=a.dtype, device=a.device)
+        whole[:, :, :K].copy_(a)
+        a = whole
+    return Adapters(a, b, scale)
+
+
 class _Plan(NamedTuple):
     ffn_ws: int
     ffn_ws_sh: int
@@ -95,12 +129,18 @@ class ExpertShardLayer:
     the intermediate dimension that is not a multiple of 64 is zero-padded once, here, and the
     FFN calls then describe the padded matrices.
     ``y_perm_bf16`` / ``out_f32`` select the element types of the intermediate and the output.
+
+    ``adapters`` are low-rank updates of the whole module, y[t] += scale_i B_i A_i x[t] for the adapter i that forward's
+    ``adapter_idx`` names for token t (outside 0 .. L-1: none); ``shared_adapters`` are those of the shared expert's down
+    projection, which read its activated rows.  Shards' outputs add up with them too: the module's belong to one shard, or
+    each shard holds some of their ranks; the down projection's are sliced along K as w_down is.
+    ``backward`` trains what is not frozen beside the experts: the router, the shared expert's gate and the module's adapters.
     """
 
     def __init__(self, *, n_experts, top_k, hidden, inter_full, inter_slice, n_local_experts=None, expert_offset=0,
                  renorm=True, w_router=None, w_gate=None, w_up=None, w_down=None, shared=None, w_shared_gate=None,
                  inter_shared_full=0, inter_shared_slice=0, max_tokens=0, y_perm_bf16=False, out_f32=False,
-                 overlap_shared=True, gather_in_ffn=None, device="cuda"):
+                 overlap_shared=True, gather_in_ffn=None, adapters=None, shared_adapters=None, device="cuda"):
         n_local_experts = n_experts if n_local_experts is None else n_local_experts
         self.E, self.k, self.H = n_experts, top_k, hidden
         self.shard = B.make_shard(n_experts, n_local_experts, expert_offset, hidden, inter_full, inter_slice)
@@ -116,6 +156,11 @@ class ExpertShardLayer:
             self.shared_shard = B.make_shard(1, 1, 0, hidden, padded * (inter_shared_full // inter_shared_slice),
                                              padded)
         self.y_perm_bf16, self.out_f32 = y_perm_bf16, out_f32
+        if shared_adapters is not None and shared is None:
+            raise ValueError("shared_adapters without a shared expert")
+        self.adapters = None if adapters is None else _adapters(adapters, hidden, hidden)
+        self.shared_adapters = (None if shared_adapters is None else
+                                _adapters(shared_adapters, inter_shared_slice, hidden, self.shared_shard.inter_slice))
         self.device = device
         # the shared expert depends on x only: it may run on a second stream (default priority) beside
         # routing, permutation and the routed experts, and joins before the combine
@@ -129,7 +174,7 @@ class ExpertShardLayer:
         self._gather_auto = gather_in_ffn is None
         self.overlap_shared = bool(overlap_shared) and shared is not None
         self._side = _side_stream(device) if self.overlap_shared else None
-        self.Tmax = -1
+        self.Tmax, self._grad_tmax = -1, -1
         # {0, T} for the shared expert's call, one immutable device tensor per token count: a
         # captured graph keeps reading the tensor it was captured with
         self._sh_offsets = {}
@@ -141,7 +186,10 @@ class ExpertShardLayer:
             self._alloc(max_tokens)
 
     _BUFFERS = ("logits", "topk_idx", "topk_w", "x_perm", "expert_offsets", "row_src", "slot_row", "h_ws", "y_perm",
-                "workspace", "ffn_ws", "y_out", "h_sh", "y_shared", "ffn_ws_sh")
+                "workspace", "ffn_ws", "y_out", "h_sh", "y_shared", "ffn_ws_sh", "lora_v", "lora_ws")
+    # of the losses and the backward pass, allocated on first use
+    _GRAD_BUFFERS = ("d_topk_w", "d_logits", "d_shared_gate", "dx", "d_w_router", "d_w_shared_gate", "grad_a", "grad_b", "counts",
+                     "mean_prob", "losses", "grad_ws")
 
     def _retire(self, names):
         if self._captured:
@@ -170,7 +218,60 @@ class ExpertShardLayer:
             self.y_shared = torch.empty((Tn, H), dtype=ydt, device=d)
             self.ffn_ws_sh = torch.empty(max(B.moe_ffn_workspace_bytes(Tn, self.shared_shard), 256),
                                          dtype=torch.uint8, device=d)
+        if self.adapters is not None:
+            self.lora_v = torch.empty((Tn, self.adapters.a.shape[1]), dtype=torch.float32, device=d)
+        if self.adapters is not None or self.shared_adapters is not None:
+            # (a call of few tokens may need more than one of more)
+            self.lora_ws = torch.empty(max(self._lora_bytes(t) for t in {Tn, min(Tn, 64)}), dtype=torch.uint8, device=d)
         self.Tmax = T
+
+    def _lora_bytes(self, T):
+        """Workspace of the adapters' forward calls, which run one after the other."""
+        need = [256]
+        for ad in (self.adapters, self.shared_adapters):
+            if ad is not None:
+                need.append(B.moe_lora_workspace_bytes(T, ad.a.shape[2], self.H, ad.a.shape[1], ad.a.shape[0]))
+        return max(need)
+
+    def _alloc_grad(self, T):
+        d, H, E, Tn = self.device, self.H, self.E, max(T, 1)
+        self._retire(self._GRAD_BUFFERS)
+        f32 = lambda *shape: torch.empty(shape, dtype=torch.float32, device=d)  # noqa: E731
+        self.d_topk_w, self.d_logits, self.d_shared_gate = f32(Tn, self.k), f32(Tn, E), f32(Tn)
+        self.dx = torch.empty((Tn, H), dtype=torch.bfloat16, device=d)
+        self.d_w_router, self.d_w_shared_gate = f32(H, E), f32(H, 1)
+        self.counts = torch.empty(E + 1, dtype=torch.int32, device=d)
+        self.mean_prob, self.losses = f32(E), f32(2)
+        if self.adapters is not None:
+            self.grad_a, self.grad_b = f32(*self.adapters.a.shape), f32(*self.adapters.b.shape)
+        self.grad_ws = torch.empty(self._grad_bytes(Tn), dtype=torch.uint8, device=d)
+        self._grad_tmax = T
+
+    def _grad_bytes(self, T):
+        """Workspace of the losses and the gradients, whose calls run one after the other."""
+        need = [256, B.moe_balance_workspace_bytes(T, self.E), B.moe_router_backward_workspace_bytes(T, self.H, self.E),
+                B.moe_router_backward_workspace_bytes(T, self.H, 1)]
+        if self.adapters is not None:
+            L, rank, _ = self.adapters.a.shape
+            need.append(B.moe_lora_workspace_bytes(T, self.H, self.H, rank, L, True))
+        return max(need)
+
+    def _room_for_grad(self, T):
+        capturing = torch.cuda.is_current_stream_capturing()
+        if T > self._grad_tmax:
+            if capturing:
+                raise RuntimeError("run one eager call with this token count before capturing a graph")
+            self._alloc_grad(T)
+        elif self._grad_bytes(T) > self.grad_ws.numel():
+            if capturing:
+                raise RuntimeError("run one eager call with this token count before capturing a graph")
+            self._retire(("grad_ws",))
+            self.grad_ws = torch.empty(self._grad_bytes(T), dtype=torch.uint8, device=self.device)
+        self._captured |= capturing
+
+    def _check_rows(self, t, name, shape, dtype):
+        if tuple(t.shape) != shape or t.dtype != dtype:
+            raise ValueError("%s: %s %s required" % (name, dtype, list(shape)))
 
     def _shared_offsets(self, T):
         """Device tensor {0, T}: written once, on first use of this token count, and complete
@@ -269,8 +370,13 @@ class ExpertShardLayer:
             self._plans[key] = plan
         return plan
 
-    def forward(self, x: torch.Tensor, logits: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    def forward(self, x: torch.Tensor, logits: torch.Tensor | None = None, stream=None,
+                adapter_idx: torch.Tensor | None = None) -> torch.Tensor:
         T = x.shape[0]
+        if adapter_idx is not None:
+            if self.adapters is None and self.shared_adapters is None:
+                raise ValueError("adapter_idx for a layer without adapters")
+            self._check_rows(adapter_idx, "adapter_idx", (T,), torch.int32)
         if T > self.Tmax:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("run one eager forward with this token count before capturing a graph")
@@ -301,8 +407,12 @@ class ExpertShardLayer:
             ptr(self.workspace), self.workspace.numel(), ptr(self.w_gate), ptr(self.w_up), ptr(self.w_down),
             ptr(self.h_ws), ptr(self.y_perm), ptr(self.ffn_ws), self.ffn_ws.numel(),
             None, ptr(gate_x), ptr(self.w_shared_gate), ptr(self.y_out), T, k, flags, yflag | plan.hint, cflags)
+        if adapter_idx is not None and self._lora_bytes(T) > self.lora_ws.numel():
+            self._retire(("lora_ws",))
+            self.lora_ws = torch.empty(self._lora_bytes(T), dtype=torch.uint8, device=self.device)
         if self.shared is None:
             B.moe_forward(args, self.shard, self.ffn_shard, stream)
+            self._add_adapters(x, adapter_idx, T, stream)
             return self.y_out[:T]
         args.combine_flags = B.MOE_NO_COMBINE     # the combine waits for the shared expert
         sh_offsets = self._shared_offsets(T)
@@ -317,6 +427,7 @@ class ExpertShardLayer:
                 # at once instead of waiting for a resident workgroup to finish (-2 to -3.5 % at 16 to 64 tokens)
                 B.moe_expert_ffn(x, sh_offsets, T, self.shared_shard, self.shared[0], self.shared[1], self.shared[2],
                                  self.h_sh, self.y_shared, self.ffn_ws_sh, yflag | B.MOE_FFN_LEAVE_ROOM, self._side)
+                self._add_shared_adapters(adapter_idx, T, self._side)
 
             # Eager, the shared expert first: it starts while the host enqueues the others.  A graph runs its branches in the
             # order of their first kernels and the combine on the first one's queue, so there the routed experts, where they
@@ -332,16 +443,93 @@ class ExpertShardLayer:
             B.moe_forward(args, self.shard, self.ffn_shard, stream)
             B.moe_expert_ffn(x, sh_offsets, T, self.shared_shard, self.shared[0], self.shared[1], self.shared[2],
                              self.h_sh, self.y_shared, self.ffn_ws_sh, yflag, stream)
+            self._add_shared_adapters(adapter_idx, T, stream)
         B.moe_combine(self.y_perm, self.slot_row, self.topk_w, T, k, H, self.y_shared, gate_x, self.w_shared_gate,
                       self.y_out, cflags, stream)
+        self._add_adapters(x, adapter_idx, T, stream)
         return self.y_out[:T]
 
-    def capture(self, x: torch.Tensor, logits: torch.Tensor | None = None):
+    def _add_adapters(self, x, adapter_idx, T, stream):
+        if adapter_idx is None or self.adapters is None:
+            return
+        L, rank, _ = self.adapters.a.shape
+        B.moe_lora_forward(x, adapter_idx, T, self.H, self.H, rank, L, *self.adapters, self.y_out, self.y_out, self.lora_v,
+                           self.lora_ws, B.MOE_OUT_F32 if self.out_f32 else 0, stream)
+
+    def _add_shared_adapters(self, adapter_idx, T, stream):
+        """Beside the shared expert's down projection, from the rows that it read."""
+        if adapter_idx is None or self.shared_adapters is None:
+            return
+        L, rank, K = self.shared_adapters.a.shape
+        B.moe_lora_forward(self.h_sh, adapter_idx, T, K, self.H, rank, L, *self.shared_adapters, self.y_shared, self.y_shared, None,
+                           self.lora_ws, 0 if self.y_perm_bf16 else B.MOE_OUT_F32, stream)
+
+    def router_losses(self, token_mask: torch.Tensor | None = None, stream=None):
+        """The last forward's balance and z loss (a device tensor of two) and its rows per expert ([E] int32, then the tokens that
+        count: those of token_mask, uint8, that are not 0)."""
+        T = self._last_T
+        if token_mask is not None:
+            self._check_rows(token_mask, "token_mask", (T,), torch.uint8)
+        self._room_for_grad(T)
+        B.moe_balance_loss(self.logits, self.topk_idx, token_mask, T, self.E, self.k, self.counts, self.mean_prob, self.losses,
+                           self.grad_ws, stream)
+        return self.losses, self.counts
+
+    def backward(self, x: torch.Tensor, dy: torch.Tensor, adapter_idx: torch.Tensor | None = None,
+                 token_mask: torch.Tensor | None = None, coef_balance: float = 0.0, coef_z: float = 0.0,
+                 dx_in: torch.Tensor | None = None, need_dx: bool = True, stream=None) -> Gradients:
+        """Gradients of the last forward, of the same x and adapter_idx, for dy [T,H] bf16 and the router's losses times their
+        coefficients.  The experts' own weights are frozen.  dx holds what reaches x through the router, the shared expert's
+        gate and the module's adapters, added to dx_in, the part through the experts.  A shard's gradients are its part of a
+        sum: those of all shards, the losses' coefficients given to one of them, add up to the unsharded layer's."""
+        T, H, E = self._last_T, self.H, self.E
+        self._check_rows(x, "x", (T, H), torch.bfloat16)
+        self._check_rows(dy, "dy", (T, H), torch.bfloat16)
+        if adapter_idx is not None:
+            if self.adapters is None:
+                raise ValueError("adapter_idx for a layer without adapters")
+            if self.shared_adapters is not None:
+                raise ValueError("the adapters of the shared expert's down projection are served, not trained")
+            self._check_rows(adapter_idx, "adapter_idx", (T,), torch.int32)
+        if dx_in is not None:
+            self._check_rows(dx_in, "dx_in", (T, H), torch.bfloat16)
+            if not need_dx:
+                raise ValueError("dx_in without dx")
+        self._room_for_grad(T)
+        gate = self.w_shared_gate is not None and self.shared is not None
+        B.moe_combine_backward(dy, self.y_perm, self.slot_row, T, self.k, H, self.y_shared if gate else None, x if gate else None,
+                               self.w_shared_gate if gate else None, self.d_topk_w, self.d_shared_gate if gate else None,
+                               B.MOE_Y_PERM_BF16 if self.y_perm_bf16 else 0, stream)
+        losses = coef_balance != 0.0 or coef_z != 0.0
+        if losses:
+            self.router_losses(token_mask, stream)
+        B.moe_route_backward(self.logits, self.topk_idx, self.d_topk_w, token_mask, self.counts if losses else None, T, E, self.k,
+                             coef_balance, coef_z, B.MOE_RENORM_TOPK if self.renorm else 0, self.d_logits, stream)
+        dx = self.dx if need_dx else None
+        if self.w_router is not None:
+            B.moe_router_backward(x, self.w_router, self.d_logits, T, H, E, dx_in, dx, self.d_w_router, self.grad_ws, stream)
+            dx_in = dx
+        if gate:
+            B.moe_router_backward(x, self.w_shared_gate, self.d_shared_gate, T, H, 1, dx_in, dx, self.d_w_shared_gate, self.grad_ws,
+                                  stream)
+            dx_in = dx
+        if adapter_idx is not None:
+            L, rank, _ = self.adapters.a.shape
+            B.moe_lora_backward(x, dy, adapter_idx, T, H, H, rank, L, *self.adapters, self.lora_v, dx_in, dx, self.grad_a,
+                                self.grad_b, self.grad_ws, stream)
+            dx_in = dx
+        if need_dx and dx_in is not dx:   # logits from outside and nothing else that reads x
+            dx = dx_in
+        return Gradients(None if dx is None else dx[:T], self.d_logits[:T], self.d_w_router if self.w_router is not None else None,
+                         self.d_w_shared_gate[:, 0] if gate else None, self.grad_a if adapter_idx is not None else None,
+                         self.grad_b if adapter_idx is not None else None)
+
+    def capture(self, x: torch.Tensor, logits: torch.Tensor | None = None, adapter_idx: torch.Tensor | None = None):
         """Capture one forward on (x, logits) into a HIP graph; returns (graph, output view).
         Decode-sized layers are a chain of short kernels, so replaying a graph removes most of
         the launch gaps.  The library enqueues kernels only (no memset nodes, no allocation),
-        which is what makes the capture legal; x / logits are read in place at every replay."""
-        self.forward(x, logits)  # eager warm-up: sizes the buffers, sets the shared-expert offsets
+        which is what makes the capture legal; x / logits / adapter_idx are read in place at every replay."""
+        self.forward(x, logits, adapter_idx=adapter_idx)  # eager warm-up: sizes the buffers, sets the shared-expert offsets
         torch.cuda.synchronize()
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
@@ -349,7 +537,7 @@ class ExpertShardLayer:
         self._captured = True
         with torch.cuda.stream(side):
             with torch.cuda.graph(graph, stream=side):
-                out = self.forward(x, logits)
+                out = self.forward(x, logits, adapter_idx=adapter_idx)
         torch.cuda.current_stream().wait_stream(side)
         return graph, out
 
