@@ -221,9 +221,9 @@ void launch_expand_few(const ExpandFew& e, hipStream_t s) {
 // ---- sorted rows ---------------------------------------------------------------------------------------------------------------
 template <typename YT, int SPLIT>
 void launch_expand(const Expand& e, int n_tiles, hipStream_t s) {
-  if (e.r <= 32) launch_expand_kernel<YT, SPLIT, 1, 1, 8>(e, n_tiles, s);
-  else if (e.r <= 64) launch_expand_kernel<YT, SPLIT, 1, 2, 8>(e, n_tiles, s);
-  else launch_expand_kernel<YT, SPLIT, 1, 4, SPLIT == 2 ? 8 : 4>(e, n_tiles, s);  // (three parts: fewer columns, for the registers)
+  if (e.r <= 32) launch_expand_kernel<YT, SPLIT, 1, 8>(e, n_tiles, s);
+  else if (e.r <= 64) launch_expand_kernel<YT, SPLIT, 2, 8>(e, n_tiles, s);
+  else launch_expand_kernel<YT, SPLIT, 4, SPLIT == 2 ? 8 : 4>(e, n_tiles, s);  // (three parts: fewer columns, for the registers)
 }
 
 // Before the products of a backward pass, in one launch: out[c][r] = in[r][c] for A and B of each adapter that has rows, 64 x 64 values a
@@ -418,15 +418,22 @@ int moe_lora_backward(const void* x_bf16, const void* dy_bf16, const int32_t* ad
     hipLaunchKernelGGL(pack_kernel, dim3(2 * p.n_tiles), dim3(kPackThreads), 0, s,
                        Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, nullptr, 2, dx != nullptr ? packed : nullptr,
                             outer_u});
-    if (dx != nullptr)
-      launch_expand<uint16_t, 2>(Expand{tiles, list, T, n_adapters, packed, rank, a_t, rank, K, dx_in, dx}, p.n_tiles, s);
   }
   float* const partial = at<float>(ws, p.partial);
   const Outer o{at<Tile>(ws, p.pieces), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0), offsets, list, T, n_adapters,
                 {{x, outer_u, nullptr, grad_a, partial, K, ceil_div(K, kOuterCols), false},
                  {dy, outer_v, scale, grad_b, partial + (size_t)p.slots * rank * K, N, ceil_div(N, kOuterCols), true}},
                 rank, p.chunk};
-  launch_outer(o, p.n_pieces, p.slots > 0, s);
+  if (dx != nullptr && T > 0) {
+    const Expand e{tiles, list, T, n_adapters, at<u32x4>(ws, p.packed), rank, at<uint16_t>(ws, p.at), rank, K, dx_in, dx};
+    if (rank <= 16) launch_both<1, 1, 1, 8>(o, p.n_pieces, e, p.n_tiles, s);
+    else if (rank <= 32) launch_both<2, 1, 1, 8>(o, p.n_pieces, e, p.n_tiles, s);
+    else if (rank <= 64) launch_both<4, 1, 2, 8>(o, p.n_pieces, e, p.n_tiles, s);
+    else launch_both<4, 1, 4, 8>(o, p.n_pieces, e, p.n_tiles, s);
+  } else {
+    launch_outer(o, p.n_pieces, s);
+  }
+  if (p.slots > 0) launch_reduce(o, s);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

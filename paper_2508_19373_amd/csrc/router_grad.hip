@@ -587,16 +587,18 @@ int moe_router_backward(const void* x_bf16, const float* w_router, const float* 
                   ceil_div(H, kOuterCols), true},
                  {}},
                 E, p.chunk};
-  launch_outer(o, p.pieces, p.slots > 0, s);
   if (dx != nullptr && T > 0) {
     const Expand e{nullptr, nullptr, T, 1, packed, E, split, 2 * R, H, dx_in, dx};
-    const int tiles = p.tiles;
     // M_a's fragments in registers: fewer columns a wavefront for more experts
-    if (R == 32) launch_expand_kernel<uint16_t, 2, 2, 1, 8>(e, tiles, s);
-    else if (R == 64) launch_expand_kernel<uint16_t, 2, 2, 2, 8>(e, tiles, s);
-    else if (R <= 128) launch_expand_kernel<uint16_t, 2, 2, 4, 4>(e, tiles, s);
-    else launch_expand_kernel<uint16_t, 2, 2, 8, 2>(e, tiles, s);
+    if (E <= 16) launch_both<1, 2, 1, 8>(o, p.pieces, e, p.tiles, s);
+    else if (E <= 32) launch_both<2, 2, 1, 8>(o, p.pieces, e, p.tiles, s);
+    else if (E <= 64) launch_both<4, 2, 2, 8>(o, p.pieces, e, p.tiles, s);
+    else if (E <= 128) launch_both<4, 2, 4, 4>(o, p.pieces, e, p.tiles, s);
+    else launch_both<4, 2, 8, 2>(o, p.pieces, e, p.tiles, s);
+  } else {
+    launch_outer(o, p.pieces, s);
   }
+  if (p.slots > 0) launch_reduce(o, s);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

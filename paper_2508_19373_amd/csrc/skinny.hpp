@@ -512,16 +512,14 @@ __device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, int N, 
   }
 }
 
+constexpr int kExpandCols = kExpandWaves * 16;  // of a workgroup, times NJ
+
 template <typename YT, int SPLIT, int PARTS, int CH, int NJ>
-__global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e, int n_tiles) {
+__device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int which, int32_t* s_rows, char* s_buf) {
   constexpr int BYTES = NJ * (int)sizeof(YT) < 16 ? NJ * (int)sizeof(YT) : 16, W = BYTES / (int)sizeof(YT), UNITS = NJ / W;
   constexpr int COLS = 16 * NJ, U = kTileRows / 16;
   typedef uint32_t unit __attribute__((ext_vector_type(BYTES / 4)));
-  __shared__ int32_t s_rows[kTileRows];
-  __shared__ __align__(16) char s_buf[kExpandWaves * COLS * 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, q = lane >> 4;
-  const int which = blockIdx.z * gridDim.y + blockIdx.y;
-  if (which >= n_tiles) return;
   Tile tile{0, which * kTileRows, 0, which};
   if (e.tiles != nullptr) tile = e.tiles[which];
   else tile.rows = min(kTileRows, e.T - tile.first);
@@ -532,10 +530,10 @@ __global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e, int
   }
   __syncthreads();
   if (tile.group == e.L) {
-    copy_rows<YT>(e.y_in, e.y_out, e.N, s_rows, tile.rows, blockIdx.x * kExpandWaves * COLS, kExpandWaves * COLS);
+    copy_rows<YT>(e.y_in, e.y_out, e.N, s_rows, tile.rows, col_block * kExpandWaves * COLS, kExpandWaves * COLS);
     return;
   }
-  const int nbase = (blockIdx.x * kExpandWaves + wave) * COLS;
+  const int nbase = (col_block * kExpandWaves + wave) * COLS;
   if (nbase >= e.N) return;
   const int chunks = (e.r + 31) / 32;
   const YT* in = static_cast<const YT*>(e.y_in);
@@ -633,11 +631,19 @@ __global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e, int
   }
 }
 
-template <typename YT, int SPLIT, int PARTS, int CH, int NJ>
+template <typename YT, int SPLIT, int CH, int NJ>
+__global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e, int n_tiles) {
+  __shared__ int32_t s_rows[kTileRows];
+  __shared__ __align__(16) char s_buf[kExpandCols * NJ * 64];
+  const int which = blockIdx.z * gridDim.y + blockIdx.y;
+  if (which < n_tiles) expand_tile<YT, SPLIT, 1, CH, NJ>(e, blockIdx.x, which, s_rows, s_buf);
+}
+
+template <typename YT, int SPLIT, int CH, int NJ>
 void launch_expand_kernel(const Expand& e, int n_tiles, hipStream_t s) {
   constexpr int kMaxY = 32768;  // (a grid's y is 16 bits)
-  hipLaunchKernelGGL((expand_kernel<YT, SPLIT, PARTS, CH, NJ>),
-                     dim3(ceil_div(e.N, kExpandWaves * 16 * NJ), n_tiles < kMaxY ? n_tiles : kMaxY, ceil_div(n_tiles, kMaxY)),
+  hipLaunchKernelGGL((expand_kernel<YT, SPLIT, CH, NJ>),
+                     dim3(ceil_div(e.N, kExpandCols * NJ), n_tiles < kMaxY ? n_tiles : kMaxY, ceil_div(n_tiles, kMaxY)),
                      dim3(kExpandThreads), 0, s, e, n_tiles);
 }
 
@@ -666,17 +672,18 @@ struct Outer {
 
 constexpr int kOuterWaves = 4, kOuterThreads = kOuterWaves * 64, kOuterCols = 128, kMaxChunk = 4096;
 
+constexpr int kOuterBytes = kOuterWaves * 16 * (kOuterCols + 4) * 4;
+
 template <int MT>
-__global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
-  __shared__ __align__(16) char s_buf[kOuterWaves * 16 * (kOuterCols + 4) * 4];
-  static_assert(sizeof(s_buf) >= kMaxChunk * 4, "the rows' numbers lie where the sums are joined later");
+__device__ __forceinline__ void outer_tile(const Outer& o, int tile_of_cols, int piece, int part_of_r, char* s_buf) {
+  static_assert(kOuterBytes >= kMaxChunk * 4, "the rows' numbers lie where the sums are joined later");
   int32_t* const s_rows = reinterpret_cast<int32_t*>(s_buf);
   float(*const red)[16][kOuterCols + 4] = reinterpret_cast<float(*)[16][kOuterCols + 4]>(s_buf);
-  const bool second = blockIdx.x >= (unsigned)o.side[0].tiles;
+  const bool second = tile_of_cols >= o.side[0].tiles;
   const OuterSide sd = second ? o.side[1] : o.side[0];
-  const int col_tile = second ? blockIdx.x - o.side[0].tiles : blockIdx.x;
-  Tile tile{0, (int)blockIdx.y * o.chunk, 0, (int)blockIdx.y * (o.chunk / 32)};
-  if (o.pieces != nullptr) tile = o.pieces[blockIdx.y];
+  const int col_tile = second ? tile_of_cols - o.side[0].tiles : tile_of_cols;
+  Tile tile{0, piece * o.chunk, 0, piece * (o.chunk / 32)};
+  if (o.pieces != nullptr) tile = o.pieces[piece];
   else tile.rows = min(o.chunk, o.T - tile.first);
   if (tile.group < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, q = lane >> 4;
@@ -684,7 +691,7 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
     for (int i = tid; i < tile.rows; i += kOuterThreads) s_rows[i] = o.list[tile.first + i];
     __syncthreads();
   }
-  const int r = o.r, tiles = (r + 15) / 16, m0 = blockIdx.z * MT, c0 = col_tile * kOuterCols;
+  const int r = o.r, tiles = (r + 15) / 16, m0 = part_of_r * MT, c0 = col_tile * kOuterCols;
   f32x4 acc[MT][8];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -748,7 +755,7 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[m][j] = mfma(late[m - FIRST][s], f[j], acc[m][j]);
   }
-  const int slot = o.pieces != nullptr ? o.slots[blockIdx.y] : (o.T > o.chunk ? (int)blockIdx.y : -1);
+  const int slot = o.pieces != nullptr ? o.slots[piece] : (o.T > o.chunk ? piece : -1);
   const float scale = sd.scale != nullptr ? sd.scale[tile.group] : 1.f;
   float* out = slot >= 0 ? sd.part + (size_t)slot * r * sd.cols : sd.out + (size_t)tile.group * r * sd.cols;
 #pragma unroll
@@ -800,6 +807,33 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
   }
 }
 
+template <int MT>
+__global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
+  __shared__ __align__(16) char s_buf[kOuterBytes];
+  outer_tile<MT>(o, blockIdx.x, blockIdx.y, blockIdx.z, s_buf);
+}
+
+// The products of a backward pass in one launch: neither needs the other, so the end of the one is the other's beginning.
+// Workgroups are numbered through: outer's (x fastest), then expand's.
+struct Both {
+  Outer o;
+  Expand e;
+  int outer_x, pieces, outers, expand_x;
+};
+template <int MT, int PARTS, int CH, int NJ>
+__global__ __launch_bounds__(kOuterThreads, 2) void both_kernel(Both a) {
+  static_assert(kOuterThreads == kExpandThreads, "one block size");
+  constexpr int BYTES = kExpandCols * NJ * 64;
+  __shared__ int32_t s_rows[kTileRows];
+  __shared__ __align__(16) char s_buf[BYTES > kOuterBytes ? BYTES : kOuterBytes];
+  const int b = blockIdx.x;
+  if (b < a.outers) {
+    outer_tile<MT>(a.o, b % a.outer_x, b / a.outer_x % a.pieces, b / a.outer_x / a.pieces, s_buf);
+  } else {
+    expand_tile<uint16_t, 2, PARTS, CH, NJ>(a.e, (b - a.outers) % a.expand_x, (b - a.outers) / a.expand_x, s_rows, s_buf);
+  }
+}
+
 // Adds the pieces of cut groups in order.  blockIdx.y: the group; four pieces in flight.
 static __global__ __launch_bounds__(256) void reduce_kernel(Outer o) {
   const int g = blockIdx.y;
@@ -824,20 +858,29 @@ static __global__ __launch_bounds__(256) void reduce_kernel(Outer o) {
   }
 }
 
+// (More workgroups than a grid's x has room for would need 250 GB of rows.)
+template <int MT, int PARTS, int CH, int NJ>
+void launch_both(const Outer& o, int pieces, const Expand& e, int n_tiles, hipStream_t s) {
+  Both a{o, e, o.side[0].tiles + o.side[1].tiles, pieces, 0, ceil_div(e.N, kExpandCols * NJ)};
+  a.outers = a.outer_x * pieces * ceil_div(o.r, 16 * MT);
+  hipLaunchKernelGGL((both_kernel<MT, PARTS, CH, NJ>), dim3(a.outers + a.expand_x * n_tiles), dim3(kOuterThreads), 0, s, a);
+}
+
 template <int MT>
 void launch_outer_tiles(const Outer& o, int pieces, hipStream_t s) {
   hipLaunchKernelGGL(outer_kernel<MT>, dim3(o.side[0].tiles + o.side[1].tiles, pieces, ceil_div(o.r, 16 * MT)), dim3(kOuterThreads),
                      0, s, o);
 }
 
-inline void launch_outer(const Outer& o, int pieces, bool cut, hipStream_t s) {
+inline void launch_outer(const Outer& o, int pieces, hipStream_t s) {
   if (o.r <= 16) launch_outer_tiles<1>(o, pieces, s);
   else if (o.r <= 32) launch_outer_tiles<2>(o, pieces, s);
   else launch_outer_tiles<4>(o, pieces, s);
-  if (cut) {
-    const int64_t values = (int64_t)o.r * (o.side[0].cols + o.side[1].cols);
-    hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div(values, 1024), o.L), dim3(256), 0, s, o);
-  }
+}
+
+inline void launch_reduce(const Outer& o, hipStream_t s) {
+  const int64_t values = (int64_t)o.r * (o.side[0].cols + o.side[1].cols);
+  hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div(values, 1024), o.L), dim3(256), 0, s, o);
 }
 
 // Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.
