@@ -14,9 +14,9 @@ namespace {
 using namespace skinny;
 
 // ---- up to 64 rows -------------------------------------------------------------------------------------------------------------
-// Two short kernels, bound by their latency: every workgroup looks at all ids, one a lane.  The first row of an adapter stands for all of its
-// rows, sixteen at a time; the workgroups of the others end at once.  The adapters' matrices are read straight into the MFMA's operands
-// (through LDS, as for many rows, took 7.5 and 7.2 us instead of 5.7 and 5.0 with 48 rows of 32 adapters, 4096 x 4096, rank 16).
+// A short kernel or two, bound by their latency: every workgroup looks at all ids, one a lane.  With two, the adapters' matrices are read straight
+// into the MFMA's operands (through LDS, as for many rows, took 7.5 and 7.2 us instead of 5.7 and 5.0 with 48 rows of 32 adapters, 4096 x 4096,
+// rank 16).
 constexpr int kFewRows = 64, kFewTile = 16;
 
 struct Few {
@@ -24,17 +24,31 @@ struct Few {
   int T, L;
 };
 
-// Rows of workgroup b = leader * ceil(T / 16) + part: fills s_rows, returns how many; group -1: without an adapter.
+// Sixteen rows of one adapter, or fewer, are a tile; its number follows from the first row of its adapter, which stands for them all.
+int few_tiles(int T, int L) {
+  const int groups = T < L + 1 ? T : L + 1;
+  return groups + (T - groups) / kFewTile;
+}
+
+// Rows of tile b: fills s_rows, returns how many, 0 past the last one; group -1: without an adapter.
 __device__ __forceinline__ int few_rows(const Few& f, int b, int32_t* s_rows, int& group) {
-  const int lane = threadIdx.x & (kWave - 1), parts = (f.T + kFewTile - 1) / kFewTile, leader = b / parts, first = b % parts * kFewTile;
-  int g = lane < f.T ? f.idx[lane] : -2;
-  if (lane < f.T && (unsigned)g >= (unsigned)f.L) g = -1;
-  group = (int)__builtin_amdgcn_readlane(g, leader);
-  const unsigned long long same = __ballot(g == group);
-  const int n = min((int)__popcll(same) - first, kFewTile);
-  if (__ffsll((long long)same) - 1 != leader || n <= 0) return 0;
-  const int rank = (int)__popcll(same & ((1ull << lane) - 1ull)) - first;
-  if (threadIdx.x < kWave && g == group && rank >= 0 && rank < kFewTile) s_rows[rank] = lane;
+  const int lane = threadIdx.x & (kWave - 1);
+  const bool in = lane < f.T;
+  int g = in ? f.idx[lane] : -1;
+  if ((unsigned)g >= (unsigned)f.L) g = -1;
+  const unsigned long long same = match_lanes(g + 1, in, 32 - __clz(f.L));
+  const int all = (int)__popcll(same), rank = (int)__popcll(same & ((1ull << lane) - 1ull));
+  const int tiles = in && rank == 0 ? (all + kFewTile - 1) / kFewTile : 0;
+  int end = tiles;  // tiles up to this lane's
+#pragma unroll
+  for (int d = 1; d <= kFewRows / kFewTile; ++d) end += (int)__popcll(__ballot(tiles >= d) & ((1ull << lane) - 1ull));
+  const unsigned long long owner = __ballot(b >= end - tiles && b < end);
+  if (owner == 0) return 0;
+  const int src = __ffsll((long long)owner) - 1;
+  group = (int)__builtin_amdgcn_readlane(g, src);
+  const int first = (b - (int)__builtin_amdgcn_readlane(end - tiles, src)) * kFewTile;
+  const int n = min((int)__builtin_amdgcn_readlane(all, src) - first, kFewTile);
+  if (threadIdx.x < kWave && in && g == group && rank >= first && rank < first + kFewTile) s_rows[rank - first] = lane;
   return n;
 }
 
@@ -103,6 +117,42 @@ struct ExpandFew {
   void* y_out;
 };
 
+// The wavefront's columns from its fragments of M_a, v's parts in LDS and y.
+template <typename YT, int SPLIT, int CH>
+__device__ __forceinline__ void few_out(const u32x4 (&w)[CH][4], u32x4 (&y)[sizeof(YT)], const char* s_p, int n, int nbase, size_t at,
+                                        const ExpandFew& e) {
+  constexpr int R = 32 * CH, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = SPLIT * R * 2 + 16;
+  const int lane = threadIdx.x & 63, ln = lane & 15, q = lane >> 4, c0 = nbase + q * W;
+  YT* const out = static_cast<YT*>(e.y_out);
+  f32x4 acc[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int s = SPLIT - 1; s >= 0; --s) {  // the small parts first
+      const u32x4 b = *reinterpret_cast<const u32x4*>(s_p + ln * kRowBytes + s * R * 2 + c * 64 + q * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = mfma(w[c][j], b, acc[j]);
+    }
+  if (ln >= n) return;
+#pragma unroll
+  for (int h = 0; h < UNITS; ++h) {
+    if (c0 + h * 4 * W >= e.N) break;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t d = y[h][i];
+      if constexpr (W == 8) {
+        const f32x4 a = acc[2 * h + i / 2];
+        y[h][i] = pack_bf16x2(bf16_lo(d) + a[2 * (i & 1)], bf16_hi(d) + a[2 * (i & 1) + 1]);
+      } else {
+        y[h][i] = __float_as_uint(__uint_as_float(d) + acc[h][i]);
+      }
+    }
+    *reinterpret_cast<u32x4*>(out + at + h * 4 * W) = y[h];
+  }
+}
+
 template <typename YT, int SPLIT, int CH>
 __global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e) {
   constexpr int R = 32 * CH, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = SPLIT * R * 2 + 16, ITEMS = kFewTile * (R / 8);
@@ -132,7 +182,6 @@ __global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e)
     return;
   }
   const YT* in = static_cast<const YT*>(e.y_in);
-  YT* out = static_cast<YT*>(e.y_out);
   const int c0 = nbase + q * W;
   const size_t at = (size_t)s_rows[min(ln, n - 1)] * e.N + c0;
   u32x4 y[UNITS];
@@ -166,36 +215,147 @@ __global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e)
     for (int s = 0; s < SPLIT; ++s) *reinterpret_cast<u32x4*>(s_p + i * kRowBytes + s * R * 2 + j0 * 2) = take_bf16(v);
   }
   __syncthreads();
-  f32x4 acc[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-#pragma unroll
-    for (int s = SPLIT - 1; s >= 0; --s) {  // the small parts first
-      const u32x4 b = *reinterpret_cast<const u32x4*>(s_p + ln * kRowBytes + s * R * 2 + c * 64 + q * 16);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = mfma(w[c][j], b, acc[j]);
-    }
-  if (ln >= n) return;
-#pragma unroll
-  for (int h = 0; h < UNITS; ++h) {
-    if (c0 + h * 4 * W >= e.N) break;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t d = y[h][i];
-      if constexpr (W == 8) {
-        const f32x4 a = acc[2 * h + i / 2];
-        y[h][i] = pack_bf16x2(bf16_lo(d) + a[2 * (i & 1)], bf16_hi(d) + a[2 * (i & 1) + 1]);
-      } else {
-        y[h][i] = __float_as_uint(__uint_as_float(d) + acc[h][i]);
-      }
-    }
-    *reinterpret_cast<u32x4*>(out + at + h * 4 * W) = y[h];
-  }
+  few_out<YT, SPLIT, CH>(w, y, s_p, n, nbase, at, e);
 }
 
-int few_groups(int T) { return T * ceil_div(T, kFewTile); }
+// Both products in one launch: each workgroup computes v for its 512 columns anew.  The wavefronts take an eighth of k each, all of it on
+// its way at once, 128 bytes of a row by eight neighbouring lanes and through LDS into the MFMA's operands: read as operands, 16 bytes
+// from each of 16 rows, an instruction would take 64 clocks.  Two launches / one, us, in a graph and one by one from the host: 8 rows of 8
+// adapters, 4096 x 4096, rank 16 7.3 / 7.0, 9.6 / 7.1; 2048 x 2048, rank 32, 40 adapters 7.9 / 6.7, 9.4 / 6.8.
+constexpr int kFusedWaves = 8, kFusedThreads = kFusedWaves * 64;
+
+template <typename YT, int SPLIT, int NT, int FLIGHT>
+__global__ __launch_bounds__(kFusedThreads, 2) void fused_few_kernel(ExpandFew e, const uint16_t* __restrict__ x, int K,
+                                                                     const uint16_t* __restrict__ m) {
+  constexpr int R = 32, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = SPLIT * R * 2 + 16, ITEMS = kFewTile * (R / 8);
+  constexpr int kStage = (16 + 16 * NT) * 128;
+  __shared__ int32_t s_rows[kFewTile];
+  __shared__ __align__(16) char s_p[kFewTile * kRowBytes];
+  __shared__ __align__(16) char s_stage[kFusedWaves * kStage];
+  __shared__ float red[kFusedWaves][16][NT * 16 + 1];
+  int group;
+  const int n = few_rows(e.few, blockIdx.y, s_rows, group);
+  if (n == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, q = lane >> 4, sub = lane >> 3, ch = lane & 7;
+  const int r = e.r;
+  __syncthreads();
+  if (group < 0) {
+    copy_rows<YT, kFusedThreads>(e.y_in, e.y_out, e.N, s_rows, n, blockIdx.x * kFusedWaves * 64, kFusedWaves * 64);
+    if (e.keep != nullptr && blockIdx.x == 0)
+      for (int i = tid; i < n * r; i += kFusedThreads) e.keep[(size_t)s_rows[i / r] * r + i % r] = 0.f;
+    return;
+  }
+  // (loads without conditions: past the end the last piece again, past K the first columns, both taken as zeros)
+  const int pieces = (K + 63) / 64, first = pieces * wave / kFusedWaves, count = pieces * (wave + 1) / kFusedWaves - first;
+  const uint16_t *xr[2], *mr[2 * NT];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) xr[i] = x + (size_t)s_rows[min(8 * i + sub, n - 1)] * K + 8 * ch;
+#pragma unroll
+  for (int i = 0; i < 2 * NT; ++i) mr[i] = m + ((size_t)group * r + min(8 * i + sub, r - 1)) * K + 8 * ch;
+  u32x4 xv[FLIGHT][2], mv[FLIGHT][2 * NT];
+#pragma unroll
+  for (int f = 0; f < FLIGHT; ++f) {
+    int c = (first + max(min(f, count - 1), 0)) * 64;
+    c = c + 8 * ch < K ? c : -8 * ch;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) xv[f][i] = *reinterpret_cast<const u32x4*>(xr[i] + c);
+#pragma unroll
+    for (int i = 0; i < 2 * NT; ++i) mv[f][i] = *reinterpret_cast<const u32x4*>(mr[i] + c);
+  }
+  // what the second product needs, on its way meanwhile
+  const int nbase = (blockIdx.x * kFusedWaves + wave) * 64, c0 = nbase + q * W;
+  u32x4 w[1][4], y[UNITS];
+  const size_t at = (size_t)s_rows[min(ln, n - 1)] * e.N + c0;
+  {
+    const bool some = e.y_in != nullptr;
+    const YT* const in = some ? static_cast<const YT*>(e.y_in) + (size_t)s_rows[min(ln, n - 1)] * e.N : reinterpret_cast<const YT*>(e.m);
+    const int last = some ? e.N - W : 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int col = W == 8 ? (j >> 1) * 32 + (ln >> 2) * 8 + (j & 1) * 4 + (ln & 3) : 16 * j + ln;
+      w[0][j] = *reinterpret_cast<const u32x4*>(e.m + ((size_t)group * e.N + min(nbase + col, e.N - 1)) * r + min(8 * q, r - 8));
+    }
+#pragma unroll
+    for (int h = 0; h < UNITS; ++h) y[h] = *reinterpret_cast<const u32x4*>(in + min(c0 + h * 4 * W, last));
+  }
+  const float scale = e.scale[group];
+  f32x4 acc[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  char* const s_x = s_stage + wave * kStage;
+  char* const s_m = s_x + 2048;
+  const int put = sub * 128 + (ch ^ sub) * 16;  // + 1024 for each eight rows
+#pragma unroll
+  for (int f = 0; f < FLIGHT; ++f) {
+    const bool in = f < count && (first + f) * 64 + 8 * ch < K;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 v = xv[f][i];
+      *reinterpret_cast<u32x4*>(s_x + put + 1024 * i) = u32x4{in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u};
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * NT; ++i) *reinterpret_cast<u32x4*>(s_m + put + 1024 * i) = mv[f][i];
+    wave_fence();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int from = ln * 128 + (((4 * h + q) ^ (ln & 7)) * 16);
+      const u32x4 a = *reinterpret_cast<const u32x4*>(s_x + from);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[j] = mfma(a, *reinterpret_cast<const u32x4*>(s_m + 2048 * j + from), acc[j]);
+    }
+    wave_fence();
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) red[wave][4 * q + k][16 * j + ln] = acc[j][k];
+  __syncthreads();
+  if (tid < ITEMS) {
+    const int i = tid / (R / 8), j0 = tid % (R / 8) * 8;
+    float v[8] = {};
+    if (i < n && j0 < r) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+#pragma unroll
+        for (int p = 0; p < kFusedWaves; ++p) v[k] += red[p][i][j0 + k];
+        if (e.keep != nullptr && blockIdx.x == 0) e.keep[(size_t)s_rows[i] * r + j0 + k] = v[k];
+        v[k] *= scale;
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < SPLIT; ++p) *reinterpret_cast<u32x4*>(s_p + i * kRowBytes + p * R * 2 + j0 * 2) = take_bf16(v);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (8 * q >= r) w[0][j] = u32x4{};
+  if (e.y_in == nullptr)
+#pragma unroll
+    for (int h = 0; h < UNITS; ++h) y[h] = u32x4{};
+  __syncthreads();
+  few_out<YT, SPLIT, 1>(w, y, s_p, n, nbase, at, e);
+}
+
+// Where k comes in one go (else its halves wait for each other: 2 x 256 KB, rank 32, 7.8 / 8.9 us; 2 x 88 KB of K = 5632 7.5 / 8.4), the
+// workgroups run side by side and what they read again is little: 16 / 28 MB of A 7.9 / 7.4, 7.5 / 7.3; 32 MB and 256 workgroups 8.2 / 9.8.
+constexpr int64_t kFusedBytes = 28 << 20;
+bool fused_few(int T, int K, int N, int rank, int L) {
+  const int64_t groups = (int64_t)few_tiles(T, L) * ceil_div(N, kFusedWaves * 64);
+  return rank <= 32 && K * ceil_div(rank, 16) <= 4096 && groups <= 256 && groups * K * rank * 2 <= kFusedBytes;
+}
+
+template <typename YT, int SPLIT, int NT, int FLIGHT>
+void launch_fused(const ExpandFew& e, const uint16_t* x, int K, const uint16_t* m, hipStream_t s) {
+  hipLaunchKernelGGL((fused_few_kernel<YT, SPLIT, NT, FLIGHT>), dim3(ceil_div(e.N, kFusedWaves * 64), few_tiles(e.few.T, e.few.L)),
+                     dim3(kFusedThreads), 0, s, e, x, K, m);
+}
+template <typename YT, int SPLIT>
+void launch_fused_few(const ExpandFew& e, const uint16_t* x, int K, const uint16_t* m, hipStream_t s) {
+  const int flight = ceil_div(K, 64 * kFusedWaves);
+  if (e.r > 16) launch_fused<YT, SPLIT, 2, 4>(e, x, K, m, s);
+  else if (flight <= 4) launch_fused<YT, SPLIT, 1, 4>(e, x, K, m, s);
+  else launch_fused<YT, SPLIT, 1, 8>(e, x, K, m, s);
+}
+
 // Pieces of the sum over k: 64 of k for each of the eight wavefronts, 16 at most.
 int few_pieces(int K) {
   const int n = ceil_div(K, 64 * kFewWaves);
@@ -203,7 +363,7 @@ int few_pieces(int K) {
 }
 
 void launch_shrink_few(const Few& few, const uint16_t* x, int K, const uint16_t* m, int r, float* part, hipStream_t s) {
-  const dim3 grid(few_groups(few.T), few_pieces(K)), block(kFewWaves * 64);
+  const dim3 grid(few_tiles(few.T, few.L), few_pieces(K)), block(kFewWaves * 64);
   if (r <= 16) hipLaunchKernelGGL(shrink_few_kernel<1>, grid, block, 0, s, few, x, K, m, r, part);
   else if (r <= 32) hipLaunchKernelGGL(shrink_few_kernel<2>, grid, block, 0, s, few, x, K, m, r, part);
   else if (r <= 64) hipLaunchKernelGGL(shrink_few_kernel<4>, grid, block, 0, s, few, x, K, m, r, part);
@@ -212,7 +372,7 @@ void launch_shrink_few(const Few& few, const uint16_t* x, int K, const uint16_t*
 
 template <typename YT, int SPLIT>
 void launch_expand_few(const ExpandFew& e, hipStream_t s) {
-  const dim3 grid(ceil_div(e.N, kExpandWaves * 64), few_groups(e.few.T)), block(kExpandThreads);
+  const dim3 grid(ceil_div(e.N, kExpandWaves * 64), few_tiles(e.few.T, e.few.L)), block(kExpandThreads);
   if (e.r <= 32) hipLaunchKernelGGL((expand_few_kernel<YT, SPLIT, 1>), grid, block, 0, s, e);
   else if (e.r <= 64) hipLaunchKernelGGL((expand_few_kernel<YT, SPLIT, 2>), grid, block, 0, s, e);
   else hipLaunchKernelGGL((expand_few_kernel<YT, SPLIT, 4>), grid, block, 0, s, e);
@@ -361,10 +521,15 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
   if (p.few) {
     const Few few{adapter_idx, T, n_adapters};
     float* const part = at<float>(ws, p.part);
-    launch_shrink_few(few, x, K, a, rank, part, s);
     const ExpandFew e{few, part, p.slices, rank, scale, v, b, N, y_in, y_out};
-    if (f32) launch_expand_few<float, 3>(e, s);
-    else launch_expand_few<uint16_t, 2>(e, s);
+    if (fused_few(T, K, N, rank, n_adapters)) {
+      if (f32) launch_fused_few<float, 3>(e, x, K, a, s);
+      else launch_fused_few<uint16_t, 2>(e, x, K, a, s);
+    } else {
+      launch_shrink_few(few, x, K, a, rank, part, s);
+      if (f32) launch_expand_few<float, 3>(e, s);
+      else launch_expand_few<uint16_t, 2>(e, s);
+    }
   } else {
     sort_rows(p, adapter_idx, T, n_adapters, ws, s);
     const int32_t* list = at<int32_t>(ws, p.list);

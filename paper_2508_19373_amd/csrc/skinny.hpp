@@ -487,7 +487,7 @@ struct Expand {
 };
 
 // `n` rows without a group: the output is the input.
-template <typename YT>
+template <typename YT, int THREADS = kExpandThreads>
 __device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, int N, const int32_t* s_rows, int n, int c0, int cols) {
   constexpr int W = 16 / sizeof(YT);
   const YT* in = static_cast<const YT*>(y_in);
@@ -496,18 +496,18 @@ __device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, int N, 
   if (in == out) return;
   {
     const int per_row = cols / W, total = n * per_row;
-    for (int i0 = threadIdx.x; i0 < total; i0 += 8 * kExpandThreads) {
+    for (int i0 = threadIdx.x; i0 < total; i0 += 8 * THREADS) {
       u32x4 v[8];
       size_t at[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int i = min(i0 + u * kExpandThreads, total - 1);
+        const int i = min(i0 + u * THREADS, total - 1);
         at[u] = (size_t)s_rows[i / per_row] * N + c0 + i % per_row * W;
         v[u] = in != nullptr ? *reinterpret_cast<const u32x4*>(in + at[u]) : u32x4{};
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        if (i0 + u * kExpandThreads < total) *reinterpret_cast<u32x4*>(out + at[u]) = v[u];
+        if (i0 + u * THREADS < total) *reinterpret_cast<u32x4*>(out + at[u]) = v[u];
     }
   }
 }
