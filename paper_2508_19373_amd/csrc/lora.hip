@@ -379,11 +379,20 @@ void launch_expand_few(const ExpandFew& e, hipStream_t s) {
 }
 
 // ---- sorted rows ---------------------------------------------------------------------------------------------------------------
+// Whether each workgroup that needs v adds its slices itself, which saves a launch, or pack_kernel does it once.  Once / each, us, 4096 x
+// 4096: rank 16, 300 rows 15.7 / 13.6, 8192 50.3 / 48.2; rank 64, 300 rows 19.1 / 18.3, 4096 (8 slices) 44.3 / 48.9, 8192 (4) 69 / 73.
+bool from_sums(int T, int rank, int slices) { return rank <= 32 || (rank <= 64 && T * slices <= 24576); }
+
 template <typename YT, int SPLIT>
 void launch_expand(const Expand& e, int n_tiles, hipStream_t s) {
-  if (e.r <= 32) launch_expand_kernel<YT, SPLIT, 1, 8>(e, n_tiles, s);
-  else if (e.r <= 64) launch_expand_kernel<YT, SPLIT, 2, 8>(e, n_tiles, s);
-  else launch_expand_kernel<YT, SPLIT, 4, SPLIT == 2 ? 8 : 4>(e, n_tiles, s);  // (three parts: fewer columns, for the registers)
+  if (e.packed == nullptr) {
+    if (e.r <= 32) launch_expand_kernel<YT, SPLIT, 1, 8, true>(e, n_tiles, s);
+    else launch_expand_kernel<YT, SPLIT, 2, 8, true>(e, n_tiles, s);
+  } else {
+    if (e.r <= 32) launch_expand_kernel<YT, SPLIT, 1, 8, false>(e, n_tiles, s);
+    else if (e.r <= 64) launch_expand_kernel<YT, SPLIT, 2, 8, false>(e, n_tiles, s);
+    else launch_expand_kernel<YT, SPLIT, 4, SPLIT == 2 ? 8 : 4, false>(e, n_tiles, s);  // (three parts: fewer columns, for the registers)
+  }
 }
 
 // Before the products of a backward pass, in one launch: out[c][r] = in[r][c] for A and B of each adapter that has rows, 64 x 64 values a
@@ -453,7 +462,7 @@ Plan make_plan(int T, int K, int N, int rank, int L, bool backward) {
   p.tiles = take(p.n_tiles * sizeof(Tile));
   p.packed = take(packed_bytes(p.n_tiles, rank, 3));  // (two parts for bf16 results)
   if (backward) {
-    p.chunk = outer_chunk(T, ceil_div(K, kOuterCols) + ceil_div(N, kOuterCols), rank, 512);
+    p.chunk = outer_chunk(T, L, ceil_div(K, kOuterCols) + ceil_div(N, kOuterCols), rank, 512);
     p.n_pieces = T / p.chunk + L;
     p.slots = T > p.chunk ? 2 * (T / p.chunk) : 0;
     p.pieces = take(p.n_pieces * sizeof(Tile));
@@ -537,9 +546,11 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
     float* const part = at<float>(ws, p.part);
     u32x4* const packed = at<u32x4>(ws, p.packed);
     launch_shrink(Shrink{tiles, list, T, n_adapters, x, a, K, rank, part}, p.n_tiles, p.slices, s);
-    hipLaunchKernelGGL(pack_kernel, dim3(2 * p.n_tiles), dim3(kPackThreads), 0, s,
-                       Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, v, f32 ? 3 : 2, packed, nullptr});
-    const Expand e{tiles, list, T, n_adapters, packed, rank, b, rank, N, y_in, y_out};
+    const bool sums = from_sums(T, rank, p.slices);
+    if (!sums)
+      hipLaunchKernelGGL(pack_kernel, dim3(2 * p.n_tiles), dim3(kPackThreads), 0, s,
+                         Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, v, f32 ? 3 : 2, packed, nullptr});
+    const Expand e{tiles, list, T, n_adapters, sums ? nullptr : packed, rank, b, rank, N, y_in, y_out, part, p.slices, scale, v};
     if (f32) launch_expand<float, 3>(e, p.n_tiles, s);
     else launch_expand<uint16_t, 2>(e, p.n_tiles, s);
   }

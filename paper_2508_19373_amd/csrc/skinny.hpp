@@ -484,6 +484,11 @@ struct Expand {
   int m_stride, N;
   const void* y_in;     // [T][N] or nullptr
   void* y_out;          // [T][N]
+  // FROM_SUMS: instead of `packed`, the slices of v's sum, the groups' scales and where v is kept (or nullptr)
+  const float* part;
+  int slices;
+  const float* scale;
+  float* keep;
 };
 
 // `n` rows without a group: the output is the input.
@@ -514,8 +519,9 @@ __device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, int N, 
 
 constexpr int kExpandCols = kExpandWaves * 16;  // of a workgroup, times NJ
 
-template <typename YT, int SPLIT, int PARTS, int CH, int NJ>
-__device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int which, int32_t* s_rows, char* s_buf) {
+// FROM_SUMS: the workgroup adds v's slices and splits it itself, into s_p (as launch_shrink left them, [slices][T][r]).
+template <typename YT, int SPLIT, int PARTS, int CH, int NJ, bool FROM_SUMS = false>
+__device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int which, int32_t* s_rows, char* s_buf, u32x4* s_p = nullptr) {
   constexpr int BYTES = NJ * (int)sizeof(YT) < 16 ? NJ * (int)sizeof(YT) : 16, W = BYTES / (int)sizeof(YT), UNITS = NJ / W;
   constexpr int COLS = 16 * NJ, U = kTileRows / 16;
   typedef uint32_t unit __attribute__((ext_vector_type(BYTES / 4)));
@@ -531,10 +537,12 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
   __syncthreads();
   if (tile.group == e.L) {
     copy_rows<YT>(e.y_in, e.y_out, e.N, s_rows, tile.rows, col_block * kExpandWaves * COLS, kExpandWaves * COLS);
+    if (FROM_SUMS && e.keep != nullptr && col_block == 0)
+      for (int i = tid; i < tile.rows * e.r; i += kExpandThreads) e.keep[(size_t)s_rows[i / e.r] * e.r + i % e.r] = 0.f;
     return;
   }
   const int nbase = (col_block * kExpandWaves + wave) * COLS;
-  if (nbase >= e.N) return;
+  if (!FROM_SUMS && nbase >= e.N) return;
   const int chunks = (e.r + 31) / 32;
   const YT* in = static_cast<const YT*>(e.y_in);
   YT* out = static_cast<YT*>(e.y_out);
@@ -542,15 +550,17 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
   unit y[2][4][UNITS];
   u32x4 p[2][CH][SPLIT];
   // (no load under a condition: the compiler would wait for all loads behind it)
-  const unit* const base = in != nullptr ? reinterpret_cast<const unit*>(in) : reinterpret_cast<const unit*>(e.packed);
+  const unit* const base = in != nullptr ? reinterpret_cast<const unit*>(in) : reinterpret_cast<const unit*>(e.m);
   const int in_last = in != nullptr ? e.N - W : 0;
   const size_t in_stride = in != nullptr ? e.N : 0;
   const auto load = [&](unit(&yy)[4][UNITS], u32x4(&pp)[CH][SPLIT], int u) {
-    const u32x4* const from = e.packed + ((size_t)tile.at * U + u) * chunks * SPLIT * 64 + lane;
+    if constexpr (!FROM_SUMS) {
+      const u32x4* const from = e.packed + ((size_t)tile.at * U + u) * chunks * SPLIT * 64 + lane;
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+      for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int s = 0; s < SPLIT; ++s) pp[c][s] = from[(min(c, chunks - 1) * SPLIT + s) * 64];
+        for (int s = 0; s < SPLIT; ++s) pp[c][s] = from[(min(c, chunks - 1) * SPLIT + s) * 64];
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -558,10 +568,25 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
         yy[k][h] = *reinterpret_cast<const unit*>(reinterpret_cast<const YT*>(base) + s_rows[16 * u + 4 * q + k] * in_stride +
                                                   min(c0 + 64 * h, in_last));
   };
+  // v's sums first: they are needed first, and loads return in order
+  constexpr int PER_ROW = 4 * CH, ITEMS = FROM_SUMS ? kTileRows * PER_ROW / kExpandThreads : 1, SLICES = FROM_SUMS ? 8 : 1;
+  float4 sums[ITEMS][SLICES][2];
+  if constexpr (FROM_SUMS) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int item = tid + i * kExpandThreads, j0 = min(item % PER_ROW * 8, e.r - 8);
+      const float* const from = e.part + (size_t)s_rows[item / PER_ROW] * e.r + j0;
+#pragma unroll
+      for (int p = 0; p < SLICES; ++p)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          sums[i][p][h] = *reinterpret_cast<const float4*>(from + (size_t)min(p, e.slices - 1) * e.T * e.r + 4 * h);
+    }
+  }
   // M_a: 32 columns at a time into LDS, a row's four 16-byte parts rearranged so that both sides meet few bank conflicts
   u32x4 w[PARTS][CH][NJ];
   char* const s_m = s_buf + wave * COLS * 64;
-  const uint16_t* const mr = e.m + ((size_t)tile.group * e.N + nbase) * e.m_stride;
+  const uint16_t* const mr = e.m + (size_t)tile.group * e.N * e.m_stride;
   const int m_cols = PARTS == 2 ? 32 * chunks : e.r;
 #pragma unroll
   for (int pt = 0; pt < PARTS; ++pt)
@@ -569,12 +594,42 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int i = 0; i < NJ; ++i) {
-        const int n = min(16 * i + (lane >> 2), e.N - 1 - nbase), col = 32 * c + 8 * (lane & 3);
+        const int n = min(nbase + 16 * i + (lane >> 2), e.N - 1), col = 32 * c + 8 * (lane & 3);
         w[pt][c][i] = *reinterpret_cast<const u32x4*>(mr + (size_t)n * e.m_stride + (col < m_cols ? pt * 32 * chunks + col : 0));
       }
   const int last = (tile.rows - 1) / 16;
   load(y[0], p[0], 0);
   __builtin_amdgcn_sched_barrier(0);
+  if constexpr (FROM_SUMS) {
+    const float scale = e.scale[tile.group];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int item = tid + i * kExpandThreads, row = item / PER_ROW, j0 = item % PER_ROW * 8;
+      float v[8] = {};
+      if (j0 < e.r) {
+#pragma unroll
+        for (int p = 0; p < SLICES; ++p) {
+          const bool in = p < e.slices;
+          const float4 a = sums[i][p][0], b = sums[i][p][1];
+          const float more[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] += in ? more[k] : 0.f;
+        }
+        if (e.keep != nullptr && col_block == 0 && row < tile.rows) {
+          float4* const at = reinterpret_cast<float4*>(e.keep + (size_t)s_rows[row] * e.r + j0);
+          at[0] = make_float4(v[0], v[1], v[2], v[3]);
+          at[1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= scale;
+      }
+#pragma unroll
+      for (int s = 0; s < SPLIT; ++s)
+        s_p[((row / 16 * CH + j0 / 32) * SPLIT + s) * 64 + j0 % 32 / 8 * 16 + row % 16] = take_bf16(v);
+    }
+    __syncthreads();
+    if (nbase >= e.N) return;
+  }
 #pragma unroll
   for (int pt = 0; pt < PARTS; ++pt)
 #pragma unroll
@@ -605,7 +660,7 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int s = SPLIT - 1; s >= 0; --s) {  // the small parts first
-        const u32x4 a = p[u & 1][c][s];
+        const u32x4 a = FROM_SUMS ? s_p[((u * CH + c) * SPLIT + s) * 64 + lane] : p[u & 1][c][s];
         if (PARTS == 2 && s == 0)
 #pragma unroll
           for (int j = 0; j < NJ; ++j) acc[j] = mfma(a, w[PARTS - 1][c][j], acc[j]);
@@ -631,18 +686,19 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
   }
 }
 
-template <typename YT, int SPLIT, int CH, int NJ>
+template <typename YT, int SPLIT, int CH, int NJ, bool FROM_SUMS>
 __global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e, int n_tiles) {
   __shared__ int32_t s_rows[kTileRows];
+  __shared__ u32x4 s_p[FROM_SUMS ? kTileRows / 16 * CH * SPLIT * 64 : 1];
   __shared__ __align__(16) char s_buf[kExpandCols * NJ * 64];
   const int which = blockIdx.z * gridDim.y + blockIdx.y;
-  if (which < n_tiles) expand_tile<YT, SPLIT, 1, CH, NJ>(e, blockIdx.x, which, s_rows, s_buf);
+  if (which < n_tiles) expand_tile<YT, SPLIT, 1, CH, NJ, FROM_SUMS>(e, blockIdx.x, which, s_rows, s_buf, s_p);
 }
 
-template <typename YT, int SPLIT, int CH, int NJ>
+template <typename YT, int SPLIT, int CH, int NJ, bool FROM_SUMS>
 void launch_expand_kernel(const Expand& e, int n_tiles, hipStream_t s) {
   constexpr int kMaxY = 32768;  // (a grid's y is 16 bits)
-  hipLaunchKernelGGL((expand_kernel<YT, SPLIT, CH, NJ>),
+  hipLaunchKernelGGL((expand_kernel<YT, SPLIT, CH, NJ, FROM_SUMS>),
                      dim3(ceil_div(e.N, kExpandCols * NJ), n_tiles < kMaxY ? n_tiles : kMaxY, ceil_div(n_tiles, kMaxY)),
                      dim3(kExpandThreads), 0, s, e, n_tiles);
 }
@@ -883,8 +939,12 @@ inline void launch_reduce(const Outer& o, hipStream_t s) {
   hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div(values, 1024), o.L), dim3(256), 0, s, o);
 }
 
-// Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.
-inline int outer_chunk(int T, int tiles, int r, int want) {
+// Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.  Few rows are not cut, which saves the launch that
+// adds the pieces: up to 512 of one group (2048 columns, cut / not, us: 333 rows 15.7 / 14.6, 512 15.9 / 16.3, 700 16.6 / 20.1), twice as many of
+// several groups, among which they are seldom all one's (4 groups, 777 rows 23.3 / 21.5, 1024 23.9 / 21.9; all of one group 24.0 / 25.1).
+constexpr int kUncut = 512;
+inline int outer_chunk(int T, int L, int tiles, int r, int want) {
+  if (T <= (L > 1 ? 2 * kUncut : kUncut)) return 2 * kUncut;
   const int64_t chunk = ((int64_t)T * tiles * ceil_div(r, 64) / want + 255) / 256 * 256;
   return chunk < 256 ? 256 : (chunk > kMaxChunk ? kMaxChunk : (int)chunk);
 }
