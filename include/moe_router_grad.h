@@ -9,10 +9,10 @@
  * The experts' own matrices are taken as frozen: no gradient of moe_expert_ffn is computed, and dx holds the router's part only.
  *
  * Conventions as in moe_shard.h: status codes (MOE_OK / MOE_ERR_*), validation on the host before any HIP call, no allocation, no
- * synchronisation, work enqueued on `stream`; all pointers are DEVICE pointers owned by the caller.  With T == 0 the buffers of T rows may be NULL.  bf16 tensors, y_perm,
- * y_shared, w_shared_gate, d_w_router and workspaces are 16-byte aligned.  A call writes all of its workspace that it reads, so nothing
- * has to start at zero; calls that overlap on one GPU each bring their own.  Sums are taken in a fixed order: the same call gives the
- * same bits.
+ * synchronisation, work enqueued on `stream`; all pointers are DEVICE pointers owned by the caller.  With T == 0 the buffers of T rows
+ * may be NULL.  bf16 tensors, y_perm, y_shared, w_shared_gate, d_w_router and workspaces are 16-byte aligned.  A call writes all of its
+ * workspace that it reads, so nothing has to start at zero; calls that overlap on one GPU each bring their own.  Sums are taken in a fixed
+ * order: the same call gives the same bits.
  */
 #ifndef MOE_ROUTER_GRAD_H
 #define MOE_ROUTER_GRAD_H

@@ -175,6 +175,7 @@ class ExpertShardLayer:
         self.overlap_shared = bool(overlap_shared) and shared is not None
         self._side = _side_stream(device) if self.overlap_shared else None
         self.Tmax, self._grad_tmax = -1, -1
+        self._has_v = False   # the last forward kept the module's adapters' v
         # {0, T} for the shared expert's call, one immutable device tensor per token count: a
         # captured graph keeps reading the tensor it was captured with
         self._sh_offsets = {}
@@ -268,6 +269,11 @@ class ExpertShardLayer:
             self._retire(("grad_ws",))
             self.grad_ws = torch.empty(self._grad_bytes(T), dtype=torch.uint8, device=self.device)
         self._captured |= capturing
+
+    def _rows(self):
+        if not hasattr(self, "_last_T"):
+            raise RuntimeError("run a forward first")
+        return self._last_T
 
     def _check_rows(self, t, name, shape, dtype):
         if tuple(t.shape) != shape or t.dtype != dtype:
@@ -381,7 +387,7 @@ class ExpertShardLayer:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("run one eager forward with this token count before capturing a graph")
             self._alloc(T)
-        self._last_T = T
+        self._last_T, self._has_v = T, adapter_idx is not None and self.adapters is not None
         k, H = self.k, self.H
         plan = self._plan(T)
         # the FFN scratch depends on the regime (decode-sized calls need split-K partials)
@@ -467,7 +473,7 @@ class ExpertShardLayer:
     def router_losses(self, token_mask: torch.Tensor | None = None, stream=None):
         """The last forward's balance and z loss (a device tensor of two) and its rows per expert ([E] int32, then the tokens that
         count: those of token_mask, uint8, that are not 0)."""
-        T = self._last_T
+        T = self._rows()
         if token_mask is not None:
             self._check_rows(token_mask, "token_mask", (T,), torch.uint8)
         self._room_for_grad(T)
@@ -482,7 +488,9 @@ class ExpertShardLayer:
         coefficients.  The experts' own weights are frozen.  dx holds what reaches x through the router, the shared expert's
         gate and the module's adapters, added to dx_in, the part through the experts.  A shard's gradients are its part of a
         sum: those of all shards, the losses' coefficients given to one of them, add up to the unsharded layer's."""
-        T, H, E = self._last_T, self.H, self.E
+        T, H, E = self._rows(), self.H, self.E
+        if token_mask is not None:
+            self._check_rows(token_mask, "token_mask", (T,), torch.uint8)
         self._check_rows(x, "x", (T, H), torch.bfloat16)
         self._check_rows(dy, "dy", (T, H), torch.bfloat16)
         if adapter_idx is not None:
@@ -490,6 +498,8 @@ class ExpertShardLayer:
                 raise ValueError("adapter_idx for a layer without adapters")
             if self.shared_adapters is not None:
                 raise ValueError("the adapters of the shared expert's down projection are served, not trained")
+            if not self._has_v:
+                raise ValueError("adapter_idx for a forward without")
             self._check_rows(adapter_idx, "adapter_idx", (T,), torch.int32)
         if dx_in is not None:
             self._check_rows(dx_in, "dx_in", (T, H), torch.bfloat16)

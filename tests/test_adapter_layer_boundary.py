@@ -48,9 +48,18 @@ def test_backward_and_loss_arguments():
     x, idx = torch.zeros((4, H), dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
     layer, both = _layer(adapters=_ad(H)), _layer(shared=True, adapters=_ad(H), shared_adapters=_ad(S))
     for one in (layer, both):
+        with pytest.raises(RuntimeError):
+            one.backward(x, x)
+        with pytest.raises(RuntimeError):
+            one.router_losses()
         one._last_T = 4
+    with pytest.raises(ValueError):      # the last forward was without ids
+        layer.backward(x, x, idx)
+    layer._has_v = both._has_v = True
     for wrong in (dict(dy=x.float()), dict(dy=x[:3]), dict(x=x[:, :32]), dict(adapter_idx=idx.long()), dict(adapter_idx=idx[:2]),
-                  dict(dx_in=x.float()), dict(dx_in=x[:2]), dict(dx_in=x, need_dx=False)):
+                  dict(dx_in=x.float()), dict(dx_in=x[:2]), dict(dx_in=x, need_dx=False),
+                  dict(token_mask=torch.ones(4)),
+                  dict(token_mask=torch.ones(5, dtype=torch.uint8))):
         with pytest.raises(ValueError):
             layer.backward(**{**dict(x=x, dy=x), **wrong})
     with pytest.raises(ValueError):

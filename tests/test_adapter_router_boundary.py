@@ -116,3 +116,17 @@ def test_router_and_combine_backward_refusals(lib):
         assert _call(f, COMBINE, **change) == invalid, change
     assert _call(f, COMBINE, H=60) == shape
     assert _call(f, COMBINE, T=0) == B.MOE_OK
+
+
+def test_binding_refuses_host_tensors(lib):
+    import torch
+    t = torch.zeros((8, 8), dtype=torch.bfloat16)
+    f, i = torch.zeros((8, 8)), torch.zeros(8, dtype=torch.int32)
+    for call in (lambda: B.moe_lora_forward(t, i, 8, 8, 8, 8, 1, t, t, f, t, t, None, f),
+                 lambda: B.moe_lora_backward(t, t, i, 8, 8, 8, 8, 1, t, t, f, f, None, t, f, f, f),
+                 lambda: B.moe_balance_loss(f, i, None, 8, 8, 1, i, f, f, f),
+                 lambda: B.moe_route_backward(f, i, f, None, i, 8, 8, 1, 0.0, 0.0, 0, f),
+                 lambda: B.moe_router_backward(t, f, f, 8, 8, 8, None, t, f, f),
+                 lambda: B.moe_combine_backward(t, f, i, 8, 1, 8, None, None, None, f)):
+        with pytest.raises(ValueError):
+            call()

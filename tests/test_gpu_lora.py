@@ -75,6 +75,8 @@ SIZES = [  # T, K, N, rank, adapters, order of the ids
     (65, 136, 72, 40, 4, "runs"), (64, 512, 512, 32, 3, "none"), (200, 712, 328, 16, 7, "mixed"), (333, 512, 1024, 48, 12, "runs"),
     (777, 256, 520, 112, 3, "mixed"), (1000, 1000, 136, 64, 256, "mixed"), (2049, 128, 192, 16, 9, "mixed"),
     (2500, 72, 264, 8, 1, "one"), (300, 64, 64, 128, 5, "none"),
+    (33, 2048, 1032, 32, 20, "mixed"), (64, 4096, 520, 8, 6, "runs"), (20, 4104, 264, 16, 4, "mixed"), (600, 264, 392, 32, 5, "mixed"),
+    (25000, 64, 72, 64, 3, "runs"),
 ]
 
 
