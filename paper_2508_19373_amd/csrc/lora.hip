@@ -14,9 +14,9 @@ namespace {
 using namespace skinny;
 
 // ---- up to 64 rows -------------------------------------------------------------------------------------------------------------
-// A short kernel or two, bound by their latency: every workgroup looks at all ids, one a lane.  With two, the adapters' matrices are read straight
-// into the MFMA's operands (through LDS, as for many rows, took 7.5 and 7.2 us instead of 5.7 and 5.0 with 48 rows of 32 adapters, 4096 x 4096,
-// rank 16).
+// A short kernel or two, bound by their latency: every workgroup looks at all ids, one a lane.  With two, the adapters' matrices are read
+// straight into the MFMA's operands (through LDS, as for many rows, took 7.5 and 7.2 us instead of 5.7 and 5.0 with 48 rows of 32
+// adapters, 4096 x 4096, rank 16).
 constexpr int kFewRows = 64, kFewTile = 16;
 
 struct Few {
@@ -395,42 +395,70 @@ void launch_expand(const Expand& e, int n_tiles, hipStream_t s) {
   }
 }
 
-// Before the products of a backward pass, in one launch: out[c][r] = in[r][c] for A and B of each adapter that has rows, 64 x 64 values a
-// workgroup, and v's fragments for the outer product, 32 rows a workgroup.
-struct Prepare {
+// Before the products of a backward pass: out[c][r] = in[r][c] for A and B of each adapter that has rows, 64 x 64 values by half a workgroup,
+// four times that a workgroup.  Up to kSortOnce rows each workgroup looks for its adapter among the ids itself, and so does not wait
+// for the sort, which the launch's first workgroup does meanwhile (the whole pass, 4096 x 4096, us: 777 rows of 4 adapters, rank 64 35.5 / 32.4,
+// 8192 of 8 111 / 107, 300 of 256, rank 16 129 / 133).
+struct Transpose {
   const uint16_t* in[2];
   uint16_t* out[2];
   int R[2], C[2], tiles_c[2], tiles_a, tiles, L;  // A's tiles come first
   const int32_t* offsets;
-  Pack pack;
 };
-__global__ __launch_bounds__(kPackThreads) void prepare_kernel(Prepare p) {
-  __shared__ __align__(16) char s_buf[sizeof(PackBuffer)];
-  if (blockIdx.x >= (unsigned)(p.tiles * p.L))
-    return pack_block(p.pack, blockIdx.x - p.tiles * p.L, reinterpret_cast<float*>(s_buf), kPackStride);
-  uint16_t(*const s)[66] = reinterpret_cast<uint16_t(*)[66]>(s_buf);
-  static_assert(sizeof(PackBuffer) >= 64 * 66 * 2, "");
-  const int g = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
-  if (p.offsets[g] == p.offsets[g + 1]) return;
-  const bool second = tile >= p.tiles_a;
-  const int b = second ? tile - p.tiles_a : tile, R = second ? p.R[1] : p.R[0], C = second ? p.C[1] : p.C[0];
-  const int tc = second ? p.tiles_c[1] : p.tiles_c[0], r0 = b / tc * 64, c0 = b % tc * 64;
-  const uint16_t* in = (second ? p.in[1] : p.in[0]) + (size_t)g * R * C;
-  uint16_t* out = (second ? p.out[1] : p.out[0]) + (size_t)g * R * C;
-  static_assert(kPackThreads == 64 * 8, "eight lanes a row");
-  const int i = threadIdx.x >> 3, j = (threadIdx.x & 7) * 8;
-  if (r0 + i < R && c0 + j < C) {
-    const u32x4 v = *reinterpret_cast<const u32x4*>(in + (size_t)(r0 + i) * C + c0 + j);
+constexpr int kTurnTiles = 4;
+
+__device__ __forceinline__ void transpose_block(const Transpose& p, int block, const int32_t* idx, int T) {
+  __shared__ uint16_t s_turn[2][64][66];
+  static_assert(kSortThreads == 2 * 64 * 8, "two halves, eight lanes a row");
+  const int per = (p.tiles + kTurnTiles - 1) / kTurnTiles, g = block / per, first = block % per * kTurnTiles;
+  if (idx == nullptr) {
+    if (p.offsets[g] == p.offsets[g + 1]) return;
+  } else {
+    int id[kSortSteps];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s[i][j + k] = (uint16_t)(v[k / 2] >> (16 * (k & 1)));
-  }
-  __syncthreads();
-  if (c0 + i < C && r0 + j < R) {
-    uint32_t v[4];
+    for (int u = 0; u < kSortSteps; ++u) id[u] = idx[min((int)threadIdx.x + u * kSortThreads, T - 1)];
+    bool some = false;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = s[j + 2 * k][i] | (uint32_t)s[j + 2 * k + 1][i] << 16;
-    *reinterpret_cast<u32x4*>(out + (size_t)(c0 + i) * R + r0 + j) = u32x4{v[0], v[1], v[2], v[3]};
+    for (int u = 0; u < kSortSteps; ++u) some |= id[u] == g;
+    if (!__syncthreads_or(some)) return;
   }
+  const int half = threadIdx.x >> 9, i = (threadIdx.x & 511) >> 3, j = (threadIdx.x & 7) * 8;
+  uint16_t(*const s)[66] = s_turn[half];
+#pragma unroll
+  for (int n = 0; n < kTurnTiles; n += 2) {
+    const int tile = first + n + half;
+    const bool in_range = tile < p.tiles, second = tile >= p.tiles_a;
+    const int b = second ? tile - p.tiles_a : tile, R = second ? p.R[1] : p.R[0], C = second ? p.C[1] : p.C[0];
+    const int tc = second ? p.tiles_c[1] : p.tiles_c[0], r0 = b / tc * 64, c0 = b % tc * 64;
+    const uint16_t* in = (second ? p.in[1] : p.in[0]) + (size_t)g * R * C;
+    uint16_t* out = (second ? p.out[1] : p.out[0]) + (size_t)g * R * C;
+    if (in_range && r0 + i < R && c0 + j < C) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(in + (size_t)(r0 + i) * C + c0 + j);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[i][j + k] = (uint16_t)(v[k / 2] >> (16 * (k & 1)));
+    }
+    __syncthreads();
+    if (in_range && c0 + i < C && r0 + j < R) {
+      uint32_t v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = s[j + 2 * k][i] | (uint32_t)s[j + 2 * k + 1][i] << 16;
+      *reinterpret_cast<u32x4*>(out + (size_t)(c0 + i) * R + r0 + j) = u32x4{v[0], v[1], v[2], v[3]};
+    }
+    __syncthreads();
+  }
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_and_transpose_kernel(Sort s, Transpose p) {
+  if (blockIdx.x == 0) sort_block<true>(s);
+  else transpose_block(p, blockIdx.x - 1, s.idx, s.T);
+}
+__global__ __launch_bounds__(kSortThreads) void transpose_kernel(Transpose p) { transpose_block(p, blockIdx.x, nullptr, 0); }
+
+// The fragments of u and of v, 32 rows a workgroup.
+__global__ __launch_bounds__(kPackThreads) void pack_both_kernel(Pack u, Pack v, int blocks) {
+  __shared__ __align__(16) PackBuffer s_sum;
+  const bool second = blockIdx.x >= (unsigned)blocks;
+  pack_block(second ? v : u, blockIdx.x - (second ? blocks : 0), &s_sum[0][0], kPackStride);
 }
 
 // How a call is cut, and its workspace in order: a function of its sizes.
@@ -483,16 +511,17 @@ T* at(char* ws, size_t offset) {
   return reinterpret_cast<T*>(ws + offset);
 }
 
-void sort_rows(const Plan& p, const int32_t* idx, int T, int L, char* ws, hipStream_t s) {
-  launch_sort(Sort{idx, T, L, p.chunk, p.n_tiles, p.n_pieces, at<int32_t>(ws, p.offsets), at<int32_t>(ws, p.list), at<Tile>(ws, p.tiles),
-                   at<Tile>(ws, p.pieces), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0)},
-              s);
+Sort sort_of(const Plan& p, const int32_t* idx, int T, int L, char* ws) {
+  return Sort{idx, T, L, p.chunk, p.n_tiles, p.n_pieces, at<int32_t>(ws, p.offsets), at<int32_t>(ws, p.list), at<Tile>(ws, p.tiles),
+              at<Tile>(ws, p.pieces), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0)};
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int size_status(int32_t T, int32_t K, int32_t N, int32_t rank, int32_t L) {
-  if (T < 0 || T >= (1 << 24) || K < 8 || N < 8 || K > MOE_LORA_MAX_COLUMNS || N > MOE_LORA_MAX_COLUMNS || rank < 1 || L < 1 || L > MOE_LORA_MAX_ADAPTERS) return MOE_ERR_INVALID_ARG;
+  if (T < 0 || T >= (1 << 24) || K < 8 || N < 8 || K > MOE_LORA_MAX_COLUMNS || N > MOE_LORA_MAX_COLUMNS ||
+      rank < 1 || L < 1 || L > MOE_LORA_MAX_ADAPTERS)
+    return MOE_ERR_INVALID_ARG;
   if (K % 8 != 0 || N % 8 != 0 || rank % 8 != 0 || rank > MOE_LORA_MAX_RANK) return MOE_ERR_UNSUPPORTED_SHAPE;
   return MOE_OK;
 }
@@ -540,7 +569,7 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
       else launch_expand_few<uint16_t, 2>(e, s);
     }
   } else {
-    sort_rows(p, adapter_idx, T, n_adapters, ws, s);
+    launch_sort(sort_of(p, adapter_idx, T, n_adapters, ws), s);
     const int32_t* list = at<int32_t>(ws, p.list);
     const Tile* tiles = at<Tile>(ws, p.tiles);
     float* const part = at<float>(ws, p.part);
@@ -577,23 +606,31 @@ int moe_lora_backward(const void* x_bf16, const void* dy_bf16, const int32_t* ad
   const uint16_t *x = static_cast<const uint16_t*>(x_bf16), *dy = static_cast<const uint16_t*>(dy_bf16);
   const Plan p = make_plan(T, K, N, rank, n_adapters, true);
   char* const ws = static_cast<char*>(workspace);
-  sort_rows(p, adapter_idx, T, n_adapters, ws, s);
-  const int32_t *list = at<int32_t>(ws, p.list), *offsets = at<int32_t>(ws, p.offsets);
-  const Tile* tiles = at<Tile>(ws, p.tiles);
+  const Sort sort = sort_of(p, adapter_idx, T, n_adapters, ws);
+  const int32_t *list = sort.list, *offsets = sort.offsets;
+  const Tile* tiles = sort.tiles;
   u32x4 *const outer_u = at<u32x4>(ws, p.outer_u), *const outer_v = at<u32x4>(ws, p.outer_v);
   if (T > 0) {
     const int ra = ceil_div(rank, 64), ca = ceil_div(K, 64), cb = ceil_div(N, 64);
     uint16_t *const a_t = at<uint16_t>(ws, p.at), *const b_t = at<uint16_t>(ws, p.bt);
-    const Prepare prep{{static_cast<const uint16_t*>(lora_a), static_cast<const uint16_t*>(lora_b)}, {a_t, b_t}, {rank, N}, {K, rank},
-                       {ca, ra}, ra * ca, ra * (ca + cb), n_adapters, offsets,
-                       Pack{tiles, list, T, n_adapters, v, 1, rank, true, nullptr, nullptr, 0, nullptr, outer_v}};
-    hipLaunchKernelGGL(prepare_kernel, dim3(prep.tiles * n_adapters + 2 * p.n_tiles), dim3(kPackThreads), 0, s, prep);
+    const Transpose turn{{static_cast<const uint16_t*>(lora_a), static_cast<const uint16_t*>(lora_b)}, {a_t, b_t}, {rank, N}, {K, rank},
+                         {ca, ra}, ra * ca, ra * (ca + cb), n_adapters, offsets};
+    const int blocks = ceil_div(turn.tiles, kTurnTiles) * n_adapters;
+    if (T <= kSortOnce) {
+      hipLaunchKernelGGL(sort_and_transpose_kernel, dim3(1 + blocks), dim3(kSortThreads), 0, s, sort, turn);
+    } else {
+      launch_sort(sort, s);
+      hipLaunchKernelGGL(transpose_kernel, dim3(blocks), dim3(kSortThreads), 0, s, turn);
+    }
     float* const part = at<float>(ws, p.part);
     u32x4* const packed = at<u32x4>(ws, p.packed);
     launch_shrink(Shrink{tiles, list, T, n_adapters, dy, b_t, N, rank, part}, p.n_tiles, p.slices, s);
-    hipLaunchKernelGGL(pack_kernel, dim3(2 * p.n_tiles), dim3(kPackThreads), 0, s,
+    hipLaunchKernelGGL(pack_both_kernel, dim3(4 * p.n_tiles), dim3(kPackThreads), 0, s,
                        Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, nullptr, 2, dx != nullptr ? packed : nullptr,
-                            outer_u});
+                            outer_u},
+                       Pack{tiles, list, T, n_adapters, v, 1, rank, true, nullptr, nullptr, 0, nullptr, outer_v}, 2 * p.n_tiles);
+  } else {
+    launch_sort(sort, s);
   }
   float* const partial = at<float>(ws, p.partial);
   const Outer o{at<Tile>(ws, p.pieces), at<int32_t>(ws, p.piece_slots), at<int32_t>(ws, p.slot0), offsets, list, T, n_adapters,

@@ -113,7 +113,7 @@ __device__ __forceinline__ int find_group(const int32_t* pre, int n, int v) {
 constexpr int kSortSteps = 8, kSortOnce = kSortWaves * kSortSteps * kWave;
 
 template <bool ONE>
-__global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
+__device__ __forceinline__ void sort_block(const Sort& s) {
   __shared__ int32_t cnt[kSortWaves][kMaxGroups + 1];
   __shared__ int32_t pre[5][kMaxGroups + 2];  // prefixes over the groups of rows, tiles, whole pieces, other pieces, slots
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, groups = s.L + 1, bits = 32 - __clz(s.L);
@@ -221,6 +221,11 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
     s.pieces[i] = t;
     s.slots[i] = slot;
   }
+}
+
+template <bool ONE>
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(Sort s) {
+  sort_block<ONE>(s);
 }
 
 inline void launch_sort(const Sort& a, hipStream_t s) {
