@@ -1,9 +1,10 @@
 // Low-rank adapters of many requests beside one projection: y += scale_a (x A_a^T) B_a^T with the row's own adapter a, and the
 // gradients of A, B and x.
 //
-// A decoding batch of up to 64 rows: shrink_few_kernel, expand_few_kernel.  More rows are sorted by adapter first (skinny.hpp):
+// A decoding batch of up to 64 rows: fused_few_kernel, or shrink_few_kernel and expand_few_kernel.  More rows are sorted by adapter first
+// (skinny.hpp), a launch for each product:
 //   forward:  v = shrink(x, A), y = expand(v, B)
-//   backward: u = shrink(dy, B^T), dx = expand(u, A^T), grad A = outer(u, x), grad B = outer(v, dy)
+//   backward: u = shrink(dy, B^T), then dx = expand(u, A^T), grad A = outer(u, x) and grad B = outer(v, dy) in one launch
 // B^T and A^T are written out for that: a few MB, where the products read them 16 bytes at a time along the side that is summed.
 #include "moe_lora.h"
 #include "skinny.hpp"
