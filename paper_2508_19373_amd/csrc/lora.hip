@@ -219,17 +219,17 @@ __global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e)
   few_out<YT, SPLIT, CH>(w, y, s_p, n, nbase, at, e);
 }
 
-// Both products in one launch: each workgroup computes v for its 512 columns anew.  The wavefronts take an eighth of k each, all of it on
-// its way at once, 128 bytes of a row by eight neighbouring lanes and through LDS into the MFMA's operands: read as operands, 16 bytes
+// Both products in one launch: each workgroup computes v for its 512 columns (or 1024) anew.  The wavefronts take an eighth of k each, all
+// of it on its way at once, 128 bytes of a row by eight neighbouring lanes and through LDS into the MFMA's operands: read as operands, 16 bytes
 // from each of 16 rows, an instruction would take 64 clocks.  Two launches / one, us, in a graph and one by one from the host: 8 rows of 8
 // adapters, 4096 x 4096, rank 16 7.3 / 7.0, 9.6 / 7.1; 2048 x 2048, rank 32, 40 adapters 7.9 / 6.7, 9.4 / 6.8.
 constexpr int kFusedWaves = 8, kFusedThreads = kFusedWaves * 64;
 
-template <typename YT, int SPLIT, int NT, int FLIGHT>
+template <typename YT, int SPLIT, int NT, int FLIGHT, int WIDE>
 __global__ __launch_bounds__(kFusedThreads, 2) void fused_few_kernel(ExpandFew e, const uint16_t* __restrict__ x, int K,
                                                                      const uint16_t* __restrict__ m) {
   constexpr int R = 32, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = SPLIT * R * 2 + 16, ITEMS = kFewTile * (R / 8);
-  constexpr int kStage = (16 + 16 * NT) * 128;
+  constexpr int kStage = (16 + 16 * NT) * 128, kCols = WIDE * kFusedWaves * 64;
   __shared__ int32_t s_rows[kFewTile];
   __shared__ __align__(16) char s_p[kFewTile * kRowBytes];
   __shared__ __align__(16) char s_stage[kFusedWaves * kStage];
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(kFusedThreads, 2) void fused_few_kernel(ExpandFew e
   const int r = e.r;
   __syncthreads();
   if (group < 0) {
-    copy_rows<YT, kFusedThreads>(e.y_in, e.y_out, e.N, s_rows, n, blockIdx.x * kFusedWaves * 64, kFusedWaves * 64);
+    copy_rows<YT, kFusedThreads>(e.y_in, e.y_out, e.N, s_rows, n, blockIdx.x * kCols, kCols);
     if (e.keep != nullptr && blockIdx.x == 0)
       for (int i = tid; i < n * r; i += kFusedThreads) e.keep[(size_t)s_rows[i / r] * r + i % r] = 0.f;
     return;
@@ -264,20 +264,24 @@ __global__ __launch_bounds__(kFusedThreads, 2) void fused_few_kernel(ExpandFew e
     for (int i = 0; i < 2 * NT; ++i) mv[f][i] = *reinterpret_cast<const u32x4*>(mr[i] + c);
   }
   // what the second product needs, on its way meanwhile
-  const int nbase = (blockIdx.x * kFusedWaves + wave) * 64, c0 = nbase + q * W;
-  u32x4 w[1][4], y[UNITS];
+  const int nbase = blockIdx.x * kCols + wave * 64, c0 = nbase + q * W;  // the next 64 columns of a wavefront: kFusedThreads further
+  u32x4 w[WIDE][1][4], y[WIDE][UNITS];
   const size_t at = (size_t)s_rows[min(ln, n - 1)] * e.N + c0;
   {
     const bool some = e.y_in != nullptr;
     const YT* const in = some ? static_cast<const YT*>(e.y_in) + (size_t)s_rows[min(ln, n - 1)] * e.N : reinterpret_cast<const YT*>(e.m);
     const int last = some ? e.N - W : 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int col = W == 8 ? (j >> 1) * 32 + (ln >> 2) * 8 + (j & 1) * 4 + (ln & 3) : 16 * j + ln;
-      w[0][j] = *reinterpret_cast<const u32x4*>(e.m + ((size_t)group * e.N + min(nbase + col, e.N - 1)) * r + min(8 * q, r - 8));
-    }
+    for (int i = 0; i < WIDE; ++i) {
 #pragma unroll
-    for (int h = 0; h < UNITS; ++h) y[h] = *reinterpret_cast<const u32x4*>(in + min(c0 + h * 4 * W, last));
+      for (int j = 0; j < 4; ++j) {
+        const int col = nbase + i * kFusedThreads + (W == 8 ? (j >> 1) * 32 + (ln >> 2) * 8 + (j & 1) * 4 + (ln & 3) : 16 * j + ln);
+        w[i][0][j] = *reinterpret_cast<const u32x4*>(e.m + ((size_t)group * e.N + min(col, e.N - 1)) * r + min(8 * q, r - 8));
+      }
+#pragma unroll
+      for (int h = 0; h < UNITS; ++h)
+        y[i][h] = *reinterpret_cast<const u32x4*>(in + min(c0 + i * kFusedThreads + h * 4 * W, last));
+    }
   }
   const float scale = e.scale[group];
   f32x4 acc[NT];
@@ -327,34 +331,43 @@ __global__ __launch_bounds__(kFusedThreads, 2) void fused_few_kernel(ExpandFew e
     for (int p = 0; p < SPLIT; ++p) *reinterpret_cast<u32x4*>(s_p + i * kRowBytes + p * R * 2 + j0 * 2) = take_bf16(v);
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (8 * q >= r) w[0][j] = u32x4{};
-  if (e.y_in == nullptr)
+  for (int i = 0; i < WIDE; ++i) {
 #pragma unroll
-    for (int h = 0; h < UNITS; ++h) y[h] = u32x4{};
+    for (int j = 0; j < 4; ++j)
+      if (8 * q >= r) w[i][0][j] = u32x4{};
+    if (e.y_in == nullptr)
+#pragma unroll
+      for (int h = 0; h < UNITS; ++h) y[i][h] = u32x4{};
+  }
   __syncthreads();
-  few_out<YT, SPLIT, 1>(w, y, s_p, n, nbase, at, e);
+#pragma unroll
+  for (int i = 0; i < WIDE; ++i) few_out<YT, SPLIT, 1>(w[i], y[i], s_p, n, nbase + i * kFusedThreads, at + i * kFusedThreads, e);
 }
 
 // Where k comes in one go (else its halves wait for each other: 2 x 256 KB, rank 32, 7.8 / 8.9 us; 2 x 88 KB of K = 5632 7.5 / 8.4), the
 // workgroups run side by side and what they read again is little: 16 / 28 MB of A 7.9 / 7.4, 7.5 / 7.3; 32 MB and 256 workgroups 8.2 / 9.8.
 constexpr int64_t kFusedBytes = 28 << 20;
-bool fused_few(int T, int K, int N, int rank, int L) {
-  const int64_t groups = (int64_t)few_tiles(T, L) * ceil_div(N, kFusedWaves * 64);
-  return rank <= 32 && K * ceil_div(rank, 16) <= 4096 && groups <= 256 && groups * K * rank * 2 <= kFusedBytes;
+// 512 columns a workgroup, or 1024 where that alone keeps to it (48 rows of 32 adapters, 4096 x 4096, rank 16 8.4 / 7.7, 9.4 / 7.6 from the
+// host; else narrow is faster, 24 of 24, rank 8 7.2 / 7.7).  0: two launches.
+int fused_wide(int T, int K, int N, int rank, int L) {
+  if (rank > 32 || K * ceil_div(rank, 16) > 4096) return 0;
+  for (int wide = 1; wide <= 2; ++wide) {
+    const int64_t groups = (int64_t)few_tiles(T, L) * ceil_div(N, wide * kFusedThreads);
+    if (groups <= 256 && groups * K * rank * 2 <= kFusedBytes) return wide;
+  }
+  return 0;
 }
 
 template <typename YT, int SPLIT, int NT, int FLIGHT>
-void launch_fused(const ExpandFew& e, const uint16_t* x, int K, const uint16_t* m, hipStream_t s) {
-  hipLaunchKernelGGL((fused_few_kernel<YT, SPLIT, NT, FLIGHT>), dim3(ceil_div(e.N, kFusedWaves * 64), few_tiles(e.few.T, e.few.L)),
-                     dim3(kFusedThreads), 0, s, e, x, K, m);
+void launch_fused(const ExpandFew& e, const uint16_t* x, int K, const uint16_t* m, int wide, hipStream_t s) {
+  const auto kernel = wide == 2 ? fused_few_kernel<YT, SPLIT, NT, FLIGHT, 2> : fused_few_kernel<YT, SPLIT, NT, FLIGHT, 1>;
+  hipLaunchKernelGGL(kernel, dim3(ceil_div(e.N, wide * kFusedThreads), few_tiles(e.few.T, e.few.L)), dim3(kFusedThreads), 0, s, e, x, K, m);
 }
 template <typename YT, int SPLIT>
-void launch_fused_few(const ExpandFew& e, const uint16_t* x, int K, const uint16_t* m, hipStream_t s) {
-  const int flight = ceil_div(K, 64 * kFusedWaves);
-  if (e.r > 16) launch_fused<YT, SPLIT, 2, 4>(e, x, K, m, s);
-  else if (flight <= 4) launch_fused<YT, SPLIT, 1, 4>(e, x, K, m, s);
-  else launch_fused<YT, SPLIT, 1, 8>(e, x, K, m, s);
+void launch_fused_few(const ExpandFew& e, const uint16_t* x, int K, const uint16_t* m, int wide, hipStream_t s) {
+  if (e.r > 16) launch_fused<YT, SPLIT, 2, 4>(e, x, K, m, wide, s);
+  else if (K <= 64 * kFusedWaves * 4) launch_fused<YT, SPLIT, 1, 4>(e, x, K, m, wide, s);
+  else launch_fused<YT, SPLIT, 1, 8>(e, x, K, m, wide, s);
 }
 
 // Pieces of the sum over k: 64 of k for each of the eight wavefronts, 16 at most.
@@ -561,9 +574,10 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
     const Few few{adapter_idx, T, n_adapters};
     float* const part = at<float>(ws, p.part);
     const ExpandFew e{few, part, p.slices, rank, scale, v, b, N, y_in, y_out};
-    if (fused_few(T, K, N, rank, n_adapters)) {
-      if (f32) launch_fused_few<float, 3>(e, x, K, a, s);
-      else launch_fused_few<uint16_t, 2>(e, x, K, a, s);
+    const int wide = fused_wide(T, K, N, rank, n_adapters);
+    if (wide > 0) {
+      if (f32) launch_fused_few<float, 3>(e, x, K, a, wide, s);
+      else launch_fused_few<uint16_t, 2>(e, x, K, a, wide, s);
     } else {
       launch_shrink_few(few, x, K, a, rank, part, s);
       if (f32) launch_expand_few<float, 3>(e, s);

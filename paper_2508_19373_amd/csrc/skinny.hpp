@@ -923,12 +923,20 @@ static __global__ __launch_bounds__(256) void reduce_kernel(Outer o) {
   }
 }
 
+// MT columns' tiles of P a workgroup, one at a time where the launch is thin all the same: shorter steps, and what Z's rows are read again for
+// comes from L2 (2048 columns, 60 wide, 333 rows 14.6 / 12.2 us, 700 16.7 / 15.5, 3000 (768 workgroups) 23.9 / 27.9).
+constexpr int kThin = 256;
 // (More workgroups than a grid's x has room for would need 250 GB of rows.)
 template <int MT, int PARTS, int CH, int NJ>
-void launch_both(const Outer& o, int pieces, const Expand& e, int n_tiles, hipStream_t s) {
-  Both a{o, e, o.side[0].tiles + o.side[1].tiles, pieces, 0, ceil_div(e.N, kExpandCols * NJ)};
-  a.outers = a.outer_x * pieces * ceil_div(o.r, 16 * MT);
+void launch_both_tiles(Both a, int n_tiles, hipStream_t s) {
+  a.outers = a.outer_x * a.pieces * ceil_div(a.o.r, 16 * MT);
   hipLaunchKernelGGL((both_kernel<MT, PARTS, CH, NJ>), dim3(a.outers + a.expand_x * n_tiles), dim3(kOuterThreads), 0, s, a);
+}
+template <int MT, int PARTS, int CH, int NJ>
+void launch_both(const Outer& o, int pieces, const Expand& e, int n_tiles, hipStream_t s) {
+  const Both a{o, e, o.side[0].tiles + o.side[1].tiles, pieces, 0, ceil_div(e.N, kExpandCols * NJ)};
+  if (MT > 1 && a.outer_x * pieces * ceil_div(o.r, 16) <= kThin) launch_both_tiles<1, PARTS, CH, NJ>(a, n_tiles, s);
+  else launch_both_tiles<MT, PARTS, CH, NJ>(a, n_tiles, s);
 }
 
 template <int MT>
@@ -949,11 +957,12 @@ inline void launch_reduce(const Outer& o, hipStream_t s) {
 }
 
 // Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.  Few rows are not cut, which saves the launch that
-// adds the pieces: up to 512 of one group (2048 columns, cut / not, us: 333 rows 15.7 / 14.6, 512 15.9 / 16.3, 700 16.6 / 20.1), twice as many of
-// several groups, among which they are seldom all one's (4 groups, 777 rows 23.3 / 21.5, 1024 23.9 / 21.9; all of one group 24.0 / 25.1).
-constexpr int kUncut = 512;
+// adds the pieces: up to 512 of one group for a P of up to 32 columns, 1024 of a wider one (2048 columns, cut / not, us: 30 wide, 600 rows
+// 12.0 / 11.7, 800 12.2 / 13.2; 60 wide, 600 15.4 / 12.6, 1024 17.0 / 14.4); twice as many of several groups, among which they are seldom
+// all one's (4 groups, 64 wide, 2000 rows 36.2 / 33.8; all of one group, 4096 columns 50 / 54).
 inline int outer_chunk(int T, int L, int tiles, int r, int want) {
-  if (T <= (L > 1 ? 2 * kUncut : kUncut)) return 2 * kUncut;
+  const int uncut = (r <= 32 ? 512 : 1024) * (L > 1 ? 2 : 1);
+  if (T <= uncut) return uncut;
   const int64_t chunk = ((int64_t)T * tiles * ceil_div(r, 64) / want + 255) / 256 * 256;
   return chunk < 256 ? 256 : (chunk > kMaxChunk ? kMaxChunk : (int)chunk);
 }
