@@ -478,7 +478,8 @@ inline size_t outer_bytes(int n, int r) { return (size_t)n * 2 * ceil_div(r, 16)
 // lanes of a row read and write up to 256 bytes in a row.  M_a's fragments stay in registers; they come through the wavefront's own LDS,
 // where they are put as they lie in memory.  The next 16 rows' P and Y are on their way during a step's products.  PARTS == 2: M_a itself is
 // fp32, given as rows of two bf16 parts; the product of the two low parts (2^-17 of the whole) is left out.  4096 rows of 4096 columns,
-// bf16 in and out, rank 32: 18.5 us from packed P (3.6 TB/s), 22.5 from sums, where pack_kernel's 4 us are saved.
+// bf16 in and out, rank 32: 18.5 us from packed P (3.6 TB/s), 21.9 from sums, where pack_kernel's 4 us are saved.  (All 64 rows of Y on their way from
+// the start instead of 16 ahead took more registers and 5 % longer.)
 constexpr int kExpandThreads = 256, kExpandWaves = kExpandThreads / kWave;
 
 struct Expand {
@@ -879,7 +880,8 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
 
 // The products of a backward pass in one launch: neither needs the other, so the end of the one is the other's beginning.
 // Workgroups are numbered through: outer's (x fastest), then expand's; the two taking turns was slower (the whole pass 115 / 129 us).
-// 8192 rows, rank 64, 4096 and 4096 columns: 64.7 us for 201 MB (3.1 TB/s; apart 50 + 23); 8192 tokens of 3584, 64 experts 44.4 for 117 MB (26 + 25.6).
+// 8192 rows, rank 64, 4096 and 4096 columns: 64.7 us for 201 MB (3.1 TB/s; apart 50 + 23); 8192 tokens of 3584, 64 experts 44.3 for 117 MB
+// (26 + 25.6).
 struct Both {
   Outer o;
   Expand e;

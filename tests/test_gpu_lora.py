@@ -77,6 +77,7 @@ SIZES = [  # T, K, N, rank, adapters, order of the ids
     (2500, 72, 264, 8, 1, "one"), (300, 64, 64, 128, 5, "none"),
     (33, 2048, 1032, 32, 20, "mixed"), (64, 4096, 520, 8, 6, "runs"), (20, 4104, 264, 16, 4, "mixed"), (600, 264, 392, 32, 5, "mixed"),
     (25000, 64, 72, 64, 3, "runs"), (48, 4096, 4104, 16, 32, "mixed"), (64, 2048, 2056, 24, 64, "mixed"), (60, 2000, 2600, 8, 64, "mixed"),
+    (700, 1024, 1024, 128, 6, "mixed"), (600, 1032, 2056, 32, 9, "mixed"),
 ]
 
 

@@ -101,7 +101,8 @@ def test_excluded_experts_and_invalid_ids():
 
 
 ROUTER_SIZES = [(0, 64, 8), (1, 8, 1), (1, 2048, 60), (5, 72, 3), (64, 512, 8), (65, 200, 16), (100, 1000, 60), (333, 520, 64), (257, 264, 130),
-                (700, 136, 256), (2100, 1032, 8), (4100, 256, 60)]
+                (700, 136, 256), (2100, 1032, 8), (4100, 256, 60),
+                (5000, 2048, 60), (3000, 1032, 200), (2600, 2048, 100), (2600, 2048, 20)]
 
 
 @pytest.mark.parametrize("T,H,E", ROUTER_SIZES)
