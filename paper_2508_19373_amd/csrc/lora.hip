@@ -403,8 +403,7 @@ void launch_expand(const Expand& e, int n_tiles, hipStream_t s) {
     if (e.r <= 32) launch_expand_kernel<YT, SPLIT, 1, 8, true>(e, n_tiles, s);
     else launch_expand_kernel<YT, SPLIT, 2, 8, true>(e, n_tiles, s);
   } else {
-    if (e.r <= 32) launch_expand_kernel<YT, SPLIT, 1, 8, false>(e, n_tiles, s);
-    else if (e.r <= 64) launch_expand_kernel<YT, SPLIT, 2, 8, false>(e, n_tiles, s);
+    if (e.r <= 64) launch_expand_kernel<YT, SPLIT, 2, 8, false>(e, n_tiles, s);
     else launch_expand_kernel<YT, SPLIT, 4, SPLIT == 2 ? 8 : 4, false>(e, n_tiles, s);  // (three parts: fewer columns, for the registers)
   }
 }
