@@ -478,8 +478,8 @@ inline size_t outer_bytes(int n, int r) { return (size_t)n * 2 * ceil_div(r, 16)
 // lanes of a row read and write up to 256 bytes in a row.  M_a's fragments stay in registers; they come through the wavefront's own LDS,
 // where they are put as they lie in memory.  The next 16 rows' P and Y are on their way during a step's products.  PARTS == 2: M_a itself is
 // fp32, given as rows of two bf16 parts; the product of the two low parts (2^-17 of the whole) is left out.  4096 rows of 4096 columns,
-// bf16 in and out, rank 32: 18.5 us from packed P (3.6 TB/s), 21.9 from sums, where pack_kernel's 4 us are saved.  (All 64 rows of Y on their way from
-// the start instead of 16 ahead took more registers and 5 % longer.)
+// bf16 in and out, rank 32: 18.5 us from packed P (3.6 TB/s), 21.9 from sums, where pack_kernel's 4 us are saved.  (All 64 rows of Y on
+// their way from the start instead of 16 ahead took more registers and 5 % longer.)
 constexpr int kExpandThreads = 256, kExpandWaves = kExpandThreads / kWave;
 
 struct Expand {
@@ -880,7 +880,7 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
 
 // The products of a backward pass in one launch: neither needs the other, so the end of the one is the other's beginning.
 // Workgroups are numbered through: outer's (x fastest), then expand's; the two taking turns was slower (the whole pass 115 / 129 us).
-// 8192 rows, rank 64, 4096 and 4096 columns: 64.7 us for 201 MB (3.1 TB/s; apart 50 + 23); 8192 tokens of 3584, 64 experts 44.3 for 117 MB
+// 8192 rows, rank 64, 4096 and 4096 columns: 64.7 us for 201 MB (3.1 TB/s; apart 50 + 23); 8192 tokens of 3584, 64 experts 43.3 for 117 MB
 // (26 + 25.6).
 struct Both {
   Outer o;
@@ -958,10 +958,12 @@ inline void launch_reduce(const Outer& o, hipStream_t s) {
   hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div(values, 1024), o.L), dim3(256), 0, s, o);
 }
 
-// Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.  Few rows are not cut, which saves the launch that
-// adds the pieces: up to 512 of one group for a P of up to 32 columns, 1024 of a wider one (2048 columns, cut / not, us: 30 wide, 600 rows
-// 12.0 / 11.7, 800 12.2 / 13.2; 60 wide, 600 15.4 / 12.6, 1024 17.0 / 14.4); twice as many of several groups, among which they are seldom
-// all one's (4 groups, 64 wide, 2000 rows 36.2 / 33.8; all of one group, 4096 columns 50 / 54).
+// Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.  The router wants 256, beside which expand's
+// fill the units, and has half as many parts to join as with 512 (512 / 256, us: 8192 tokens of 3584, 64 experts 53.8 / 51.8); the
+// adapters, two sides and groups of different lengths, want 512 (8192 rows of 8, rank 64, 4096 x 4096 112 / 119).  Few rows are not cut,
+// which saves the launch that adds the pieces: up to 512 of one group for a P of up to 32 columns, 1024 of a wider one (2048 columns, cut /
+// not, us: 30 wide, 600 rows 12.0 / 11.7, 800 12.2 / 13.2; 60 wide, 600 15.4 / 12.6, 1024 17.0 / 14.4); twice as many of several
+// groups, among which they are seldom all one's (4 groups, 64 wide, 2000 rows 36.2 / 33.8; all of one group, 4096 columns 50 / 54).
 inline int outer_chunk(int T, int L, int tiles, int r, int want) {
   const int uncut = (r <= 32 ? 512 : 1024) * (L > 1 ? 2 : 1);
   if (T <= uncut) return uncut;
