@@ -593,7 +593,7 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
     if (!sums)
       hipLaunchKernelGGL(pack_kernel, dim3(2 * p.n_tiles), dim3(kPackThreads), 0, s,
                          Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, v, f32 ? 3 : 2, packed, nullptr});
-    const Expand e{tiles, list, T, n_adapters, sums ? nullptr : packed, rank, b, rank, N, y_in, y_out, part, p.slices, scale, v};
+    const Expand e{tiles, list, T, n_adapters, sums ? nullptr : packed, rank, b, N, y_in, y_out, part, p.slices, scale, v};
     if (f32) launch_expand<float, 3>(e, p.n_tiles, s);
     else launch_expand<uint16_t, 2>(e, p.n_tiles, s);
   }
@@ -652,11 +652,11 @@ int moe_lora_backward(const void* x_bf16, const void* dy_bf16, const int32_t* ad
                  {dy, outer_v, scale, grad_b, partial + (size_t)p.slots * rank * K, N, ceil_div(N, kOuterCols), true}},
                 rank, p.chunk};
   if (dx != nullptr && T > 0) {
-    const Expand e{tiles, list, T, n_adapters, at<u32x4>(ws, p.packed), rank, at<uint16_t>(ws, p.at), rank, K, dx_in, dx};
-    if (rank <= 16) launch_both<1, 1, 1, 8>(o, p.n_pieces, e, p.n_tiles, s);
-    else if (rank <= 32) launch_both<2, 1, 1, 8>(o, p.n_pieces, e, p.n_tiles, s);
-    else if (rank <= 64) launch_both<4, 1, 2, 8>(o, p.n_pieces, e, p.n_tiles, s);
-    else launch_both<4, 1, 4, 8>(o, p.n_pieces, e, p.n_tiles, s);
+    const Expand e{tiles, list, T, n_adapters, at<u32x4>(ws, p.packed), rank, at<uint16_t>(ws, p.at), K, dx_in, dx};
+    if (rank <= 16) launch_both<1, ExpandByGroup<1, 8>>(o, p.n_pieces, e, p.n_tiles, s);
+    else if (rank <= 32) launch_both<2, ExpandByGroup<1, 8>>(o, p.n_pieces, e, p.n_tiles, s);
+    else if (rank <= 64) launch_both<4, ExpandByGroup<2, 8>>(o, p.n_pieces, e, p.n_tiles, s);
+    else launch_both<4, ExpandByGroup<4, 8>>(o, p.n_pieces, e, p.n_tiles, s);
   } else {
     launch_outer(o, p.n_pieces, s);
   }

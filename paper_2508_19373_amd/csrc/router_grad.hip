@@ -378,7 +378,7 @@ struct LaunchRoute {
 };
 
 // ---- gradient of the router's product --------------------------------------------------------------------------------------
-// d_w_router is the outer product of skinny.hpp over all rows, dx its expansion, with W_r in two bf16 parts: rows [h][part][R] of R
+// d_w_router is the outer product of skinny.hpp over all rows, dx its expansion, with W_r in three bf16 parts: rows [h][part][R] of R
 // columns, E rounded up to a multiple of 32 by zeros.
 int router_width(int E) { return ceil_div(E, 32) * 32; }
 
@@ -395,10 +395,13 @@ __global__ __launch_bounds__(kPackThreads) void router_prepare_kernel(const floa
     if (i >= n) break;
     const int64_t h = i / R;
     const int e = (int)(i - h * R);
-    const float v = e < E ? w[h * E + e] : 0.f;
-    const uint32_t hi = f32_to_bf16_bits(v);
-    out[h * 2 * R + e] = (uint16_t)hi;
-    out[h * 2 * R + R + e] = (uint16_t)f32_to_bf16_bits(v - bf16_bits_to_f32(hi));
+    float v = e < E ? w[h * E + e] : 0.f;
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) {
+      const uint32_t bits = f32_to_bf16_bits(v);
+      out[(h * kParts + p) * R + e] = (uint16_t)bits;
+      v -= bf16_bits_to_f32(bits);  // exact
+    }
   }
 }
 
@@ -412,8 +415,8 @@ RouterPlan plan_router(int T, int H, int E) {
   p.pieces = T > p.chunk ? ceil_div(T, p.chunk) : 1;
   p.slots = T > p.chunk ? p.pieces : 0;
   p.tiles = ceil_div(T, kTileRows);
-  p.packed = padded((size_t)H * 2 * router_width(E) * 2);
-  p.outer = p.packed + padded(packed_bytes(p.tiles, E, 2));
+  p.packed = padded((size_t)H * kParts * router_width(E) * 2);
+  p.outer = p.packed + padded(packed_bytes(p.tiles, E, kParts));
   p.partial = p.outer + padded(outer_bytes(p.tiles, E));
   p.bytes = p.partial + padded((size_t)p.slots * H * E * sizeof(float));
   return p;
@@ -582,7 +585,7 @@ int moe_router_backward(const void* x_bf16, const float* w_router, const float* 
     const int split_blocks = dx != nullptr ? ceil_div((int64_t)H * R, kSplitValues * kPackThreads) : 0;
     hipLaunchKernelGGL(router_prepare_kernel, dim3(split_blocks + 2 * p.tiles), dim3(kPackThreads), 0, s, w_router, (int64_t)H * R, E, R, split,
                        split_blocks,
-                       Pack{nullptr, nullptr, T, 1, d_logits, 1, E, E % 4 == 0 && aligned16(d_logits), nullptr, nullptr, 2,
+                       Pack{nullptr, nullptr, T, 1, d_logits, 1, E, E % 4 == 0 && aligned16(d_logits), nullptr, nullptr, kParts,
                             dx != nullptr ? packed : nullptr, outer});
   }
   const Outer o{nullptr, nullptr, nullptr, nullptr, nullptr, T, 1,
@@ -591,13 +594,10 @@ int moe_router_backward(const void* x_bf16, const float* w_router, const float* 
                  {}},
                 E, p.chunk};
   if (dx != nullptr && T > 0) {
-    const Expand e{nullptr, nullptr, T, 1, packed, E, split, 2 * R, H, dx_in, dx};
-    // M_a's fragments in registers: fewer columns a wavefront for more experts
-    if (E <= 16) launch_both<1, 2, 1, 8>(o, p.pieces, e, p.tiles, s);
-    else if (E <= 32) launch_both<2, 2, 1, 8>(o, p.pieces, e, p.tiles, s);
-    else if (E <= 64) launch_both<4, 2, 2, 8>(o, p.pieces, e, p.tiles, s);
-    else if (E <= 128) launch_both<4, 2, 4, 4>(o, p.pieces, e, p.tiles, s);
-    else launch_both<4, 2, 8, 2>(o, p.pieces, e, p.tiles, s);
+    const ExpandF32 e{T, packed, E, split, H, static_cast<const uint16_t*>(dx_in), static_cast<uint16_t*>(dx)};
+    if (E <= 16) launch_both<1, ExpandByF32>(o, p.pieces, e, p.tiles, s);
+    else if (E <= 32) launch_both<2, ExpandByF32>(o, p.pieces, e, p.tiles, s);
+    else launch_both<4, ExpandByF32>(o, p.pieces, e, p.tiles, s);
   } else {
     launch_outer(o, p.pieces, s);
   }

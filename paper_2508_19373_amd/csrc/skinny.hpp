@@ -476,9 +476,7 @@ inline size_t outer_bytes(int n, int r) { return (size_t)n * 2 * ceil_div(r, 16)
 // A wavefront computes up to 64 rows of 16 NJ columns, 16 rows at a time.  The MFMA's first operand is P, its second M_a; accumulator j of
 // lane c stands for column NJ c + j (of fp32 results 4 c + j % 4 of every 64), so that a lane's values of one row are neighbours and the 16
 // lanes of a row read and write up to 256 bytes in a row.  M_a's fragments stay in registers; they come through the wavefront's own LDS,
-// where they are put as they lie in memory.  The next 16 rows' P and Y are on their way during a step's products.  PARTS == 2: M_a itself is
-// fp32, given as rows of two bf16 parts; the product of the two low parts (2^-17 of the whole) is left out.  4096 rows of 4096 columns,
-// bf16 in and out, rank 32: 18.5 us from packed P (3.6 TB/s), 21.9 from sums, where pack_kernel's 4 us are saved.  (All 64 rows of Y on
+// where they are put as they lie in memory.  The next 16 rows' P and Y are on their way during a step's products.  4096 rows of 4096 columns, bf16 in and out, rank 32: 18.5 us from packed P (3.6 TB/s), 21.9 from sums, where pack_kernel's 4 us are saved.  (All 64 rows of Y on
 // their way from the start instead of 16 ahead took more registers and 5 % longer.)
 constexpr int kExpandThreads = 256, kExpandWaves = kExpandThreads / kWave;
 
@@ -488,8 +486,8 @@ struct Expand {
   int T, L;
   const u32x4* packed;
   int r;
-  const uint16_t* m;    // [L][N][m_stride]
-  int m_stride, N;
+  const uint16_t* m;    // [L][N][r]
+  int N;
   const void* y_in;     // [T][N] or nullptr
   void* y_out;          // [T][N]
   // FROM_SUMS: instead of `packed`, the slices of v's sum, the groups' scales and where v is kept (or nullptr)
@@ -528,7 +526,7 @@ __device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, int N, 
 constexpr int kExpandCols = kExpandWaves * 16;  // of a workgroup, times NJ
 
 // FROM_SUMS: the workgroup adds v's slices and splits it itself, into s_p (as launch_shrink left them, [slices][T][r]).
-template <typename YT, int SPLIT, int PARTS, int CH, int NJ, bool FROM_SUMS = false>
+template <typename YT, int SPLIT, int CH, int NJ, bool FROM_SUMS = false>
 __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int which, int32_t* s_rows, char* s_buf, u32x4* s_p = nullptr) {
   constexpr int BYTES = NJ * (int)sizeof(YT) < 16 ? NJ * (int)sizeof(YT) : 16, W = BYTES / (int)sizeof(YT), UNITS = NJ / W;
   constexpr int COLS = 16 * NJ, U = kTileRows / 16;
@@ -592,19 +590,16 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
     }
   }
   // M_a: 32 columns at a time into LDS, a row's four 16-byte parts rearranged so that both sides meet few bank conflicts
-  u32x4 w[PARTS][CH][NJ];
+  u32x4 w[CH][NJ];
   char* const s_m = s_buf + wave * COLS * 64;
-  const uint16_t* const mr = e.m + (size_t)tile.group * e.N * e.m_stride;
-  const int m_cols = PARTS == 2 ? 32 * chunks : e.r;
+  const uint16_t* const mr = e.m + (size_t)tile.group * e.N * e.r;
 #pragma unroll
-  for (int pt = 0; pt < PARTS; ++pt)
+  for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int i = 0; i < NJ; ++i) {
-        const int n = min(nbase + 16 * i + (lane >> 2), e.N - 1), col = 32 * c + 8 * (lane & 3);
-        w[pt][c][i] = *reinterpret_cast<const u32x4*>(mr + (size_t)n * e.m_stride + (col < m_cols ? pt * 32 * chunks + col : 0));
-      }
+    for (int i = 0; i < NJ; ++i) {
+      const int n = min(nbase + 16 * i + (lane >> 2), e.N - 1), col = 32 * c + 8 * (lane & 3);
+      w[c][i] = *reinterpret_cast<const u32x4*>(mr + (size_t)n * e.r + (col < e.r ? col : 0));
+    }
   const int last = (tile.rows - 1) / 16;
   load(y[0], p[0], 0);
   __builtin_amdgcn_sched_barrier(0);
@@ -639,24 +634,21 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
     if (nbase >= e.N) return;
   }
 #pragma unroll
-  for (int pt = 0; pt < PARTS; ++pt)
+  for (int c = 0; c < CH; ++c) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-#pragma unroll
-      for (int i = 0; i < NJ; ++i) {  // column n: accumulator and lane
-        const int n = 16 * i + (lane >> 2);
-        const int j = sizeof(YT) == 2 ? n % NJ : (n >> 6) * 4 + (n & 3), l = sizeof(YT) == 2 ? n / NJ : (n >> 2) & 15;
-        const bool zero = 32 * c + 8 * (lane & 3) >= m_cols;
-        const u32x4 v = w[pt][c][i];
-        *reinterpret_cast<u32x4*>(s_m + (j * 16 + l) * 64 + (((lane & 3) ^ (l >> 1 & 3)) * 16)) =
-            u32x4{zero ? 0u : v.x, zero ? 0u : v.y, zero ? 0u : v.z, zero ? 0u : v.w};
-      }
-      wave_fence();
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        w[pt][c][j] = *reinterpret_cast<const u32x4*>(s_m + (j * 16 + ln) * 64 + ((q ^ (ln >> 1 & 3)) * 16));
-      wave_fence();
+    for (int i = 0; i < NJ; ++i) {  // column n: accumulator and lane
+      const int n = 16 * i + (lane >> 2);
+      const int j = sizeof(YT) == 2 ? n % NJ : (n >> 6) * 4 + (n & 3), l = sizeof(YT) == 2 ? n / NJ : (n >> 2) & 15;
+      const bool zero = 32 * c + 8 * (lane & 3) >= e.r;
+      const u32x4 v = w[c][i];
+      *reinterpret_cast<u32x4*>(s_m + (j * 16 + l) * 64 + (((lane & 3) ^ (l >> 1 & 3)) * 16)) =
+          u32x4{zero ? 0u : v.x, zero ? 0u : v.y, zero ? 0u : v.z, zero ? 0u : v.w};
     }
+    wave_fence();
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) w[c][j] = *reinterpret_cast<const u32x4*>(s_m + (j * 16 + ln) * 64 + ((q ^ (ln >> 1 & 3)) * 16));
+    wave_fence();
+  }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (16 * u >= tile.rows) break;
@@ -669,11 +661,8 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
 #pragma unroll
       for (int s = SPLIT - 1; s >= 0; --s) {  // the small parts first
         const u32x4 a = FROM_SUMS ? s_p[((u * CH + c) * SPLIT + s) * 64 + lane] : p[u & 1][c][s];
-        if (PARTS == 2 && s == 0)
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) acc[j] = mfma(a, w[PARTS - 1][c][j], acc[j]);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[j] = mfma(a, w[0][c][j], acc[j]);
+        for (int j = 0; j < NJ; ++j) acc[j] = mfma(a, w[c][j], acc[j]);
       }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -700,7 +689,7 @@ __global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e, int
   __shared__ u32x4 s_p[FROM_SUMS ? kTileRows / 16 * CH * SPLIT * 64 : 1];
   __shared__ __align__(16) char s_buf[kExpandCols * NJ * 64];
   const int which = blockIdx.z * gridDim.y + blockIdx.y;
-  if (which < n_tiles) expand_tile<YT, SPLIT, 1, CH, NJ, FROM_SUMS>(e, blockIdx.x, which, s_rows, s_buf, s_p);
+  if (which < n_tiles) expand_tile<YT, SPLIT, CH, NJ, FROM_SUMS>(e, blockIdx.x, which, s_rows, s_buf, s_p);
 }
 
 template <typename YT, int SPLIT, int CH, int NJ, bool FROM_SUMS>
@@ -709,6 +698,105 @@ void launch_expand_kernel(const Expand& e, int n_tiles, hipStream_t s) {
   hipLaunchKernelGGL((expand_kernel<YT, SPLIT, CH, NJ, FROM_SUMS>),
                      dim3(ceil_div(e.N, kExpandCols * NJ), n_tiles < kMaxY ? n_tiles : kMaxY, ceil_div(n_tiles, kMaxY)),
                      dim3(kExpandThreads), 0, s, e, n_tiles);
+}
+
+// ---- expand by an fp32 matrix --------------------------------------------------------------------------------------------------
+// The same where M is fp32 too (the router's weights) and all rows are one group.  P and M are three bf16 parts each, all 24 bits of
+// either; of the nine products of parts the three below 2^-23 of the whole are left out, so that the sums are as exact as fp32 products'.
+// A wavefront has 64 columns of all 64 rows in its accumulators and takes 32 of M's columns after the other, the next ones on their way
+// meanwhile.  P's parts lie in LDS, where the workgroup's four wavefronts share them.
+constexpr int kParts = 3;
+
+struct ExpandF32 {
+  int T;
+  const u32x4* packed;   // [tiles][4][chunks of 32 columns][kParts][64]
+  int r;
+  const uint16_t* m;     // [N][kParts][32 chunks]
+  int N;
+  const uint16_t* y_in;  // [T][N] or nullptr
+  uint16_t* y_out;       // [T][N]
+};
+constexpr int kF32Cols = 64, kF32Fragments = kTileRows / 16 * kParts;  // columns of a wavefront; P's fragments of 32 columns
+constexpr int kExpandF32Bytes = (2 * kF32Fragments + kExpandWaves * kF32Cols / 16) * 1024;
+
+__device__ __forceinline__ void expand_f32_tile(const ExpandF32& e, int col_block, int which, char* s_buf) {
+  constexpr int NJ = kF32Cols / 16, U = kTileRows / 16, ITEMS = kF32Fragments / kExpandWaves;
+  static_assert(kF32Fragments % kExpandWaves == 0, "the wavefronts bring as many fragments each");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ln = lane & 15, q = lane >> 4;
+  const int first = which * kTileRows, rows = min(kTileRows, e.T - first), chunks = (e.r + 31) / 32;
+  const int nbase = (col_block * kExpandWaves + wave) * kF32Cols, c0 = nbase + NJ * ln;
+  u32x4* const s_p = reinterpret_cast<u32x4*>(s_buf);  // two of them in turns
+  char* const s_m = s_buf + 2 * kF32Fragments * 1024 + wave * kF32Cols * 64;
+  u32x4 m[kParts][NJ], p[ITEMS];
+  const auto load = [&](int c) {
+#pragma unroll
+    for (int pt = 0; pt < kParts; ++pt)
+#pragma unroll
+      for (int i = 0; i < NJ; ++i)  // (past the last column: that one again, not stored)
+        m[pt][i] = *reinterpret_cast<const u32x4*>(
+            e.m + ((size_t)min(nbase + 16 * i + (lane >> 2), e.N - 1) * kParts + pt) * 32 * chunks + 32 * c + 8 * (lane & 3));
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int f = i * kExpandWaves + wave;
+      p[i] = e.packed[((((size_t)which * U + f / kParts) * chunks + c) * kParts + f % kParts) * 64 + lane];
+    }
+  };
+  load(0);
+  f32x4 acc[U][NJ];  // from y_in on; without it the same bytes of M again, not used (no load under a condition)
+  const bool some = e.y_in != nullptr;
+  const uint16_t* const in = some ? e.y_in + (size_t)first * e.N + min(c0, e.N - NJ) : e.m;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint2 d = *reinterpret_cast<const uint2*>(in + (some ? (size_t)min(16 * u + 4 * q + k, rows - 1) * e.N : 0));
+      acc[u][0][k] = some ? bf16_lo(d.x) : 0.f;
+      acc[u][1][k] = some ? bf16_hi(d.x) : 0.f;
+      acc[u][2][k] = some ? bf16_lo(d.y) : 0.f;
+      acc[u][3][k] = some ? bf16_hi(d.y) : 0.f;
+    }
+  for (int c = 0; c < chunks; ++c) {
+    u32x4* const parts = s_p + (c & 1) * kF32Fragments * 64;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) parts[(i * kExpandWaves + wave) * 64 + lane] = p[i];
+    u32x4 w[kParts][NJ];
+#pragma unroll
+    for (int pt = 0; pt < kParts; ++pt) {
+#pragma unroll
+      for (int i = 0; i < NJ; ++i) {  // column n: accumulator n % NJ of lane n / NJ
+        const int n = 16 * i + (lane >> 2), l = n / NJ;
+        *reinterpret_cast<u32x4*>(s_m + (n % NJ * 16 + l) * 64 + (((lane & 3) ^ (l >> 1 & 3)) * 16)) = m[pt][i];
+      }
+      wave_fence();
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) w[pt][j] = *reinterpret_cast<const u32x4*>(s_m + (j * 16 + ln) * 64 + ((q ^ (ln >> 1 & 3)) * 16));
+      wave_fence();
+    }
+    __syncthreads();  // (one is enough: `parts` is written again only after the next one)
+    if (c + 1 < chunks) load(c + 1);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (16 * u >= rows) break;
+      u32x4 a[kParts];
+#pragma unroll
+      for (int s = 0; s < kParts; ++s) a[s] = parts[(u * kParts + s) * 64 + lane];
+#pragma unroll
+      for (int sum = kParts - 1; sum >= 0; --sum)  // the small products first
+#pragma unroll
+        for (int s = sum; s >= 0; --s)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[u][j] = mfma(a[s], w[sum - s][j], acc[u][j]);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int row = 16 * u + 4 * q + k;
+      if (row >= rows || c0 >= e.N) continue;
+      *reinterpret_cast<uint2*>(e.y_out + (size_t)(first + row) * e.N + c0) =
+          make_uint2(pack_bf16x2(acc[u][0][k], acc[u][1][k]), pack_bf16x2(acc[u][2][k], acc[u][3][k]));
+    }
 }
 
 // ---- outer -------------------------------------------------------------------------------------------------------------------
@@ -882,22 +970,37 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
 // Workgroups are numbered through: outer's (x fastest), then expand's; the two taking turns was slower (the whole pass 115 / 129 us).
 // 8192 rows, rank 64, 4096 and 4096 columns: 64.7 us for 201 MB (3.1 TB/s; apart 50 + 23); 8192 tokens of 3584, 64 experts 43.3 for 117 MB
 // (26 + 25.6).
+template <int CH, int NJ>
+struct ExpandByGroup {
+  typedef Expand Args;
+  static constexpr int kCols = kExpandCols * NJ, kBytes = kExpandCols * NJ * 64;
+  static __device__ __forceinline__ void run(const Args& e, int col_block, int which, int32_t* s_rows, char* s_buf) {
+    expand_tile<uint16_t, 2, CH, NJ>(e, col_block, which, s_rows, s_buf);
+  }
+};
+struct ExpandByF32 {
+  typedef ExpandF32 Args;
+  static constexpr int kCols = kExpandWaves * kF32Cols, kBytes = kExpandF32Bytes;
+  static __device__ __forceinline__ void run(const Args& e, int col_block, int which, int32_t*, char* s_buf) {
+    expand_f32_tile(e, col_block, which, s_buf);
+  }
+};
+template <typename EXPAND>
 struct Both {
   Outer o;
-  Expand e;
+  typename EXPAND::Args e;
   int outer_x, pieces, outers, expand_x;
 };
-template <int MT, int PARTS, int CH, int NJ>
-__global__ __launch_bounds__(kOuterThreads, 2) void both_kernel(Both a) {
+template <int MT, typename EXPAND>
+__global__ __launch_bounds__(kOuterThreads, 2) void both_kernel(Both<EXPAND> a) {
   static_assert(kOuterThreads == kExpandThreads, "one block size");
-  constexpr int BYTES = kExpandCols * NJ * 64;
   __shared__ int32_t s_rows[kTileRows];
-  __shared__ __align__(16) char s_buf[BYTES > kOuterBytes ? BYTES : kOuterBytes];
+  __shared__ __align__(16) char s_buf[EXPAND::kBytes > kOuterBytes ? EXPAND::kBytes : kOuterBytes];
   const int b = blockIdx.x;
   if (b < a.outers) {
     outer_tile<MT>(a.o, b % a.outer_x, b / a.outer_x % a.pieces, b / a.outer_x / a.pieces, s_buf);
   } else {
-    expand_tile<uint16_t, 2, PARTS, CH, NJ>(a.e, (b - a.outers) % a.expand_x, (b - a.outers) / a.expand_x, s_rows, s_buf);
+    EXPAND::run(a.e, (b - a.outers) % a.expand_x, (b - a.outers) / a.expand_x, s_rows, s_buf);
   }
 }
 
@@ -929,16 +1032,16 @@ static __global__ __launch_bounds__(256) void reduce_kernel(Outer o) {
 // comes from L2 (2048 columns, 60 wide, 333 rows 14.6 / 12.2 us, 700 16.7 / 15.5, 3000 (768 workgroups) 23.9 / 27.9).
 constexpr int kThin = 256;
 // (More workgroups than a grid's x has room for would need 250 GB of rows.)
-template <int MT, int PARTS, int CH, int NJ>
-void launch_both_tiles(Both a, int n_tiles, hipStream_t s) {
+template <int MT, typename EXPAND>
+void launch_both_tiles(Both<EXPAND> a, int n_tiles, hipStream_t s) {
   a.outers = a.outer_x * a.pieces * ceil_div(a.o.r, 16 * MT);
-  hipLaunchKernelGGL((both_kernel<MT, PARTS, CH, NJ>), dim3(a.outers + a.expand_x * n_tiles), dim3(kOuterThreads), 0, s, a);
+  hipLaunchKernelGGL((both_kernel<MT, EXPAND>), dim3(a.outers + a.expand_x * n_tiles), dim3(kOuterThreads), 0, s, a);
 }
-template <int MT, int PARTS, int CH, int NJ>
-void launch_both(const Outer& o, int pieces, const Expand& e, int n_tiles, hipStream_t s) {
-  const Both a{o, e, o.side[0].tiles + o.side[1].tiles, pieces, 0, ceil_div(e.N, kExpandCols * NJ)};
-  if (MT > 1 && a.outer_x * pieces * ceil_div(o.r, 16) <= kThin) launch_both_tiles<1, PARTS, CH, NJ>(a, n_tiles, s);
-  else launch_both_tiles<MT, PARTS, CH, NJ>(a, n_tiles, s);
+template <int MT, typename EXPAND>
+void launch_both(const Outer& o, int pieces, const typename EXPAND::Args& e, int n_tiles, hipStream_t s) {
+  const Both<EXPAND> a{o, e, o.side[0].tiles + o.side[1].tiles, pieces, 0, ceil_div(e.N, EXPAND::kCols)};
+  if (MT > 1 && a.outer_x * pieces * ceil_div(o.r, 16) <= kThin) launch_both_tiles<1, EXPAND>(a, n_tiles, s);
+  else launch_both_tiles<MT, EXPAND>(a, n_tiles, s);
 }
 
 template <int MT>
