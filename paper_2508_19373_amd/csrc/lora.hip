@@ -119,10 +119,10 @@ struct ExpandFew {
 };
 
 // The wavefront's columns from its fragments of M_a, v's parts in LDS and y.
-template <typename YT, int SPLIT, int CH>
+template <typename YT, int CH>
 __device__ __forceinline__ void few_out(const u32x4 (&w)[CH][4], u32x4 (&y)[sizeof(YT)], const char* s_p, int n, int nbase, size_t at,
                                         const ExpandFew& e) {
-  constexpr int R = 32 * CH, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = SPLIT * R * 2 + 16;
+  constexpr int R = 32 * CH, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = kParts * R * 2 + 16;
   const int lane = threadIdx.x & 63, ln = lane & 15, q = lane >> 4, c0 = nbase + q * W;
   YT* const out = static_cast<YT*>(e.y_out);
   f32x4 acc[4];
@@ -131,7 +131,7 @@ __device__ __forceinline__ void few_out(const u32x4 (&w)[CH][4], u32x4 (&y)[size
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int s = SPLIT - 1; s >= 0; --s) {  // the small parts first
+    for (int s = kParts - 1; s >= 0; --s) {  // the small parts first
       const u32x4 b = *reinterpret_cast<const u32x4*>(s_p + ln * kRowBytes + s * R * 2 + c * 64 + q * 16);
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[j] = mfma(w[c][j], b, acc[j]);
@@ -154,9 +154,9 @@ __device__ __forceinline__ void few_out(const u32x4 (&w)[CH][4], u32x4 (&y)[size
   }
 }
 
-template <typename YT, int SPLIT, int CH>
+template <typename YT, int CH>
 __global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e) {
-  constexpr int R = 32 * CH, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = SPLIT * R * 2 + 16, ITEMS = kFewTile * (R / 8);
+  constexpr int R = 32 * CH, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = kParts * R * 2 + 16, ITEMS = kFewTile * (R / 8);
   __shared__ int32_t s_rows[kFewTile];
   __shared__ __align__(16) char s_p[kFewTile * kRowBytes];
   static_assert(ITEMS <= kExpandThreads, "a thread has eight values of v at most");
@@ -213,10 +213,10 @@ __global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e)
       }
     }
 #pragma unroll
-    for (int s = 0; s < SPLIT; ++s) *reinterpret_cast<u32x4*>(s_p + i * kRowBytes + s * R * 2 + j0 * 2) = take_bf16(v);
+    for (int s = 0; s < kParts; ++s) *reinterpret_cast<u32x4*>(s_p + i * kRowBytes + s * R * 2 + j0 * 2) = take_bf16(v);
   }
   __syncthreads();
-  few_out<YT, SPLIT, CH>(w, y, s_p, n, nbase, at, e);
+  few_out<YT, CH>(w, y, s_p, n, nbase, at, e);
 }
 
 // Both products in one launch: each workgroup computes v for its 512 columns (or 1024) anew.  The wavefronts take an eighth of k each, all
@@ -225,10 +225,10 @@ __global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e)
 // adapters, 4096 x 4096, rank 16 7.3 / 7.0, 9.6 / 7.1; 2048 x 2048, rank 32, 40 adapters 7.9 / 6.7, 9.4 / 6.8.
 constexpr int kFusedWaves = 8, kFusedThreads = kFusedWaves * 64;
 
-template <typename YT, int SPLIT, int NT, int FLIGHT, int WIDE>
+template <typename YT, int NT, int FLIGHT, int WIDE>
 __global__ __launch_bounds__(kFusedThreads, 2) void fused_few_kernel(ExpandFew e, const uint16_t* __restrict__ x, int K,
                                                                      const uint16_t* __restrict__ m) {
-  constexpr int R = 32, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = SPLIT * R * 2 + 16, ITEMS = kFewTile * (R / 8);
+  constexpr int R = 32, W = 16 / sizeof(YT), UNITS = 64 / (4 * W), kRowBytes = kParts * R * 2 + 16, ITEMS = kFewTile * (R / 8);
   constexpr int kStage = (16 + 16 * NT) * 128, kCols = WIDE * kFusedWaves * 64;
   __shared__ int32_t s_rows[kFewTile];
   __shared__ __align__(16) char s_p[kFewTile * kRowBytes];
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(kFusedThreads, 2) void fused_few_kernel(ExpandFew e
       }
     }
 #pragma unroll
-    for (int p = 0; p < SPLIT; ++p) *reinterpret_cast<u32x4*>(s_p + i * kRowBytes + p * R * 2 + j0 * 2) = take_bf16(v);
+    for (int p = 0; p < kParts; ++p) *reinterpret_cast<u32x4*>(s_p + i * kRowBytes + p * R * 2 + j0 * 2) = take_bf16(v);
   }
 #pragma unroll
   for (int i = 0; i < WIDE; ++i) {
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(kFusedThreads, 2) void fused_few_kernel(ExpandFew e
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < WIDE; ++i) few_out<YT, SPLIT, 1>(w[i], y[i], s_p, n, nbase + i * kFusedThreads, at + i * kFusedThreads, e);
+  for (int i = 0; i < WIDE; ++i) few_out<YT, 1>(w[i], y[i], s_p, n, nbase + i * kFusedThreads, at + i * kFusedThreads, e);
 }
 
 // Where k comes in one go (else its halves wait for each other: 2 x 256 KB, rank 32, 7.8 / 8.9 us; 2 x 88 KB of K = 5632 7.5 / 8.4), the
@@ -358,16 +358,16 @@ int fused_wide(int T, int K, int N, int rank, int L) {
   return 0;
 }
 
-template <typename YT, int SPLIT, int NT, int FLIGHT>
+template <typename YT, int NT, int FLIGHT>
 void launch_fused(const ExpandFew& e, const uint16_t* x, int K, const uint16_t* m, int wide, hipStream_t s) {
-  const auto kernel = wide == 2 ? fused_few_kernel<YT, SPLIT, NT, FLIGHT, 2> : fused_few_kernel<YT, SPLIT, NT, FLIGHT, 1>;
+  const auto kernel = wide == 2 ? fused_few_kernel<YT, NT, FLIGHT, 2> : fused_few_kernel<YT, NT, FLIGHT, 1>;
   hipLaunchKernelGGL(kernel, dim3(ceil_div(e.N, wide * kFusedThreads), few_tiles(e.few.T, e.few.L)), dim3(kFusedThreads), 0, s, e, x, K, m);
 }
-template <typename YT, int SPLIT>
+template <typename YT>
 void launch_fused_few(const ExpandFew& e, const uint16_t* x, int K, const uint16_t* m, int wide, hipStream_t s) {
-  if (e.r > 16) launch_fused<YT, SPLIT, 2, 4>(e, x, K, m, wide, s);
-  else if (K <= 64 * kFusedWaves * 4) launch_fused<YT, SPLIT, 1, 4>(e, x, K, m, wide, s);
-  else launch_fused<YT, SPLIT, 1, 8>(e, x, K, m, wide, s);
+  if (e.r > 16) launch_fused<YT, 2, 4>(e, x, K, m, wide, s);
+  else if (K <= 64 * kFusedWaves * 4) launch_fused<YT, 1, 4>(e, x, K, m, wide, s);
+  else launch_fused<YT, 1, 8>(e, x, K, m, wide, s);
 }
 
 // Pieces of the sum over k: 64 of k for each of the eight wavefronts, 16 at most.
@@ -384,12 +384,12 @@ void launch_shrink_few(const Few& few, const uint16_t* x, int K, const uint16_t*
   else hipLaunchKernelGGL(shrink_few_kernel<8>, grid, block, 0, s, few, x, K, m, r, part);
 }
 
-template <typename YT, int SPLIT>
+template <typename YT>
 void launch_expand_few(const ExpandFew& e, hipStream_t s) {
   const dim3 grid(ceil_div(e.N, kExpandWaves * 64), few_tiles(e.few.T, e.few.L)), block(kExpandThreads);
-  if (e.r <= 32) hipLaunchKernelGGL((expand_few_kernel<YT, SPLIT, 1>), grid, block, 0, s, e);
-  else if (e.r <= 64) hipLaunchKernelGGL((expand_few_kernel<YT, SPLIT, 2>), grid, block, 0, s, e);
-  else hipLaunchKernelGGL((expand_few_kernel<YT, SPLIT, 4>), grid, block, 0, s, e);
+  if (e.r <= 32) hipLaunchKernelGGL((expand_few_kernel<YT, 1>), grid, block, 0, s, e);
+  else if (e.r <= 64) hipLaunchKernelGGL((expand_few_kernel<YT, 2>), grid, block, 0, s, e);
+  else hipLaunchKernelGGL((expand_few_kernel<YT, 4>), grid, block, 0, s, e);
 }
 
 // ---- sorted rows ---------------------------------------------------------------------------------------------------------------
@@ -397,14 +397,14 @@ void launch_expand_few(const ExpandFew& e, hipStream_t s) {
 // 4096: rank 16, 300 rows 15.7 / 13.6, 8192 50.3 / 48.2; rank 64, 300 rows 19.1 / 18.3, 4096 (8 slices) 44.3 / 48.9, 8192 (4) 69 / 73.
 bool from_sums(int T, int rank, int slices) { return rank <= 32 || (rank <= 64 && T * slices <= 24576); }
 
-template <typename YT, int SPLIT>
+template <typename YT>
 void launch_expand(const Expand& e, int n_tiles, hipStream_t s) {
   if (e.packed == nullptr) {
-    if (e.r <= 32) launch_expand_kernel<YT, SPLIT, 1, 8, true>(e, n_tiles, s);
-    else launch_expand_kernel<YT, SPLIT, 2, 8, true>(e, n_tiles, s);
+    if (e.r <= 32) launch_expand_kernel<YT, 1, 8, true>(e, n_tiles, s);
+    else launch_expand_kernel<YT, 2, 8, true>(e, n_tiles, s);
   } else {
-    if (e.r <= 64) launch_expand_kernel<YT, SPLIT, 2, 8, false>(e, n_tiles, s);
-    else launch_expand_kernel<YT, SPLIT, 4, SPLIT == 2 ? 8 : 4, false>(e, n_tiles, s);  // (three parts: fewer columns, for the registers)
+    if (e.r <= 64) launch_expand_kernel<YT, 2, 8, false>(e, n_tiles, s);
+    else launch_expand_kernel<YT, 4, 4, false>(e, n_tiles, s);  // (fewer columns, for the registers)
   }
 }
 
@@ -501,7 +501,7 @@ Plan make_plan(int T, int K, int N, int rank, int L, bool backward) {
   p.offsets = take((L + 2) * sizeof(int32_t));
   p.list = take((size_t)T * sizeof(int32_t));
   p.tiles = take(p.n_tiles * sizeof(Tile));
-  p.packed = take(packed_bytes(p.n_tiles, rank, 3));  // (two parts for bf16 results)
+  p.packed = take(packed_bytes(p.n_tiles, rank));
   if (backward) {
     p.chunk = outer_chunk(T, L, ceil_div(K, kOuterCols) + ceil_div(N, kOuterCols), rank, 512);
     p.n_pieces = T / p.chunk + L;
@@ -575,12 +575,12 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
     const ExpandFew e{few, part, p.slices, rank, scale, v, b, N, y_in, y_out};
     const int wide = fused_wide(T, K, N, rank, n_adapters);
     if (wide > 0) {
-      if (f32) launch_fused_few<float, 3>(e, x, K, a, wide, s);
-      else launch_fused_few<uint16_t, 2>(e, x, K, a, wide, s);
+      if (f32) launch_fused_few<float>(e, x, K, a, wide, s);
+      else launch_fused_few<uint16_t>(e, x, K, a, wide, s);
     } else {
       launch_shrink_few(few, x, K, a, rank, part, s);
-      if (f32) launch_expand_few<float, 3>(e, s);
-      else launch_expand_few<uint16_t, 2>(e, s);
+      if (f32) launch_expand_few<float>(e, s);
+      else launch_expand_few<uint16_t>(e, s);
     }
   } else {
     launch_sort(sort_of(p, adapter_idx, T, n_adapters, ws), s);
@@ -592,10 +592,10 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
     const bool sums = from_sums(T, rank, p.slices);
     if (!sums)
       hipLaunchKernelGGL(pack_kernel, dim3(2 * p.n_tiles), dim3(kPackThreads), 0, s,
-                         Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, v, f32 ? 3 : 2, packed, nullptr});
+                         Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, v, packed, nullptr});
     const Expand e{tiles, list, T, n_adapters, sums ? nullptr : packed, rank, b, N, y_in, y_out, part, p.slices, scale, v};
-    if (f32) launch_expand<float, 3>(e, p.n_tiles, s);
-    else launch_expand<uint16_t, 2>(e, p.n_tiles, s);
+    if (f32) launch_expand<float>(e, p.n_tiles, s);
+    else launch_expand<uint16_t>(e, p.n_tiles, s);
   }
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
@@ -640,9 +640,8 @@ int moe_lora_backward(const void* x_bf16, const void* dy_bf16, const int32_t* ad
     u32x4* const packed = at<u32x4>(ws, p.packed);
     launch_shrink(Shrink{tiles, list, T, n_adapters, dy, b_t, N, rank, part}, p.n_tiles, p.slices, s);
     hipLaunchKernelGGL(pack_both_kernel, dim3(4 * p.n_tiles), dim3(kPackThreads), 0, s,
-                       Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, nullptr, 2, dx != nullptr ? packed : nullptr,
-                            outer_u},
-                       Pack{tiles, list, T, n_adapters, v, 1, rank, true, nullptr, nullptr, 0, nullptr, outer_v}, 2 * p.n_tiles);
+                       Pack{tiles, list, T, n_adapters, part, p.slices, rank, true, scale, nullptr, dx != nullptr ? packed : nullptr, outer_u},
+                       Pack{tiles, list, T, n_adapters, v, 1, rank, true, nullptr, nullptr, nullptr, outer_v}, 2 * p.n_tiles);
   } else {
     launch_sort(sort, s);
   }
@@ -656,7 +655,7 @@ int moe_lora_backward(const void* x_bf16, const void* dy_bf16, const int32_t* ad
     if (rank <= 16) launch_both<1, ExpandByGroup<1, 8>>(o, p.n_pieces, e, p.n_tiles, s);
     else if (rank <= 32) launch_both<2, ExpandByGroup<1, 8>>(o, p.n_pieces, e, p.n_tiles, s);
     else if (rank <= 64) launch_both<4, ExpandByGroup<2, 8>>(o, p.n_pieces, e, p.n_tiles, s);
-    else launch_both<4, ExpandByGroup<4, 8>>(o, p.n_pieces, e, p.n_tiles, s);
+    else launch_both<4, ExpandByGroup<4, 4>>(o, p.n_pieces, e, p.n_tiles, s);
   } else {
     launch_outer(o, p.n_pieces, s);
   }

@@ -416,7 +416,7 @@ RouterPlan plan_router(int T, int H, int E) {
   p.slots = T > p.chunk ? p.pieces : 0;
   p.tiles = ceil_div(T, kTileRows);
   p.packed = padded((size_t)H * kParts * router_width(E) * 2);
-  p.outer = p.packed + padded(packed_bytes(p.tiles, E, kParts));
+  p.outer = p.packed + padded(packed_bytes(p.tiles, E));
   p.partial = p.outer + padded(outer_bytes(p.tiles, E));
   p.bytes = p.partial + padded((size_t)p.slots * H * E * sizeof(float));
   return p;
@@ -585,7 +585,7 @@ int moe_router_backward(const void* x_bf16, const float* w_router, const float* 
     const int split_blocks = dx != nullptr ? ceil_div((int64_t)H * R, kSplitValues * kPackThreads) : 0;
     hipLaunchKernelGGL(router_prepare_kernel, dim3(split_blocks + 2 * p.tiles), dim3(kPackThreads), 0, s, w_router, (int64_t)H * R, E, R, split,
                        split_blocks,
-                       Pack{nullptr, nullptr, T, 1, d_logits, 1, E, E % 4 == 0 && aligned16(d_logits), nullptr, nullptr, kParts,
+                       Pack{nullptr, nullptr, T, 1, d_logits, 1, E, E % 4 == 0 && aligned16(d_logits), nullptr, nullptr,
                             dx != nullptr ? packed : nullptr, outer});
   }
   const Outer o{nullptr, nullptr, nullptr, nullptr, nullptr, T, 1,

@@ -4,8 +4,8 @@
 //   expand  Y[t,n] = Y_in[t,n] + sum_j P[t,j] M_a[n,j]  a sum over the narrow side
 //   outer   G_a[j,c] = sum over the rows t of group a of P[t,j] Z[t,c]
 // All of them are bound by the one pass over X, Y or Z; the matrix cores do the sums (16x16x32 bf16, fp32 accumulators) with room to
-// spare, so that the narrow fp32 operand P may go in as a sum of bf16 parts: two keep 16 bits of it (enough under a bf16 result's
-// 8), three all 24 (for fp32 results).  The long operand is bf16 as it is, so nothing of it is lost.
+// spare, so that the narrow fp32 operand P goes in as a sum of three bf16 parts, all 24 bits of it.  The long operand is bf16 as it is, so
+// nothing of it is lost either.
 //
 // How the long side is read decides the speed: an MFMA's lanes l, l + 1, ... hold different rows, and a load in that order takes the address
 // unit 64 clocks an instruction (a lane at a time) instead of 16.  So neighbouring lanes read neighbouring 16 bytes of a row, and either
@@ -54,6 +54,8 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
   v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
+
+constexpr int kParts = 3;  // bf16 parts of an fp32 operand
 
 inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 inline size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -391,9 +393,8 @@ struct Pack {
   bool vec;             // rows of `part` are made of whole 16-byte pieces
   const float* scale;   // per group, for `packed` and `outer`; or nullptr
   float* keep;          // [T][r] the sums as they are, zeros for rows without a group; or nullptr
-  int split;            // parts of `packed`
-  u32x4* packed;        // for expand: [tiles][4][chunks of 32 columns][split][64]; or nullptr
-  u32x4* outer;         // for outer: [tiles][2][tiles of 16 columns][3][64]; or nullptr
+  u32x4* packed;        // for expand: [tiles][4][chunks of 32 columns][kParts][64]; or nullptr
+  u32x4* outer;         // for outer: [tiles][2][tiles of 16 columns][kParts][64]; or nullptr
 };
 constexpr int kPackThreads = 512, kPackStride = 132;
 typedef float PackBuffer[32][kPackStride];
@@ -446,8 +447,9 @@ __device__ __forceinline__ void pack_block(const Pack& a, int b, float* s_sum, i
       load8(s_sum + (16 * h + (l & 15)) * stride + 32 * c + 8 * (l >> 4), v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] *= scale;
-      u32x4* const to = a.packed + ((((size_t)t.at * 4 + 2 * half + h) * chunks + c) * a.split) * 64 + l;
-      for (int s = 0; s < a.split; ++s) to[s * 64] = take_bf16(v);
+      u32x4* const to = a.packed + ((((size_t)t.at * 4 + 2 * half + h) * chunks + c) * kParts) * 64 + l;
+#pragma unroll
+      for (int s = 0; s < kParts; ++s) to[s * 64] = take_bf16(v);
     }
   if (a.outer != nullptr) {
     const int tiles = (r + 15) / 16;
@@ -456,9 +458,9 @@ __device__ __forceinline__ void pack_block(const Pack& a, int b, float* s_sum, i
       float v[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = scale * s_sum[(8 * (l >> 4) + k) * stride + 16 * m + (l & 15)];
-      u32x4* const to = a.outer + ((size_t)t.at * 2 + half) * tiles * 3 * 64 + m * 3 * 64 + l;
+      u32x4* const to = a.outer + ((size_t)t.at * 2 + half) * tiles * kParts * 64 + m * kParts * 64 + l;
 #pragma unroll
-      for (int s = 0; s < 3; ++s) to[s * 64] = take_bf16(v);
+      for (int s = 0; s < kParts; ++s) to[s * 64] = take_bf16(v);
     }
   }
 }
@@ -469,8 +471,8 @@ static __global__ __launch_bounds__(kPackThreads) void pack_kernel(Pack a) {
 }
 
 // Bytes of both forms for n tiles.
-inline size_t packed_bytes(int n, int r, int split) { return (size_t)n * 4 * ceil_div(r, 32) * split * 1024; }
-inline size_t outer_bytes(int n, int r) { return (size_t)n * 2 * ceil_div(r, 16) * 3 * 1024; }
+inline size_t packed_bytes(int n, int r) { return (size_t)n * 4 * ceil_div(r, 32) * kParts * 1024; }
+inline size_t outer_bytes(int n, int r) { return (size_t)n * 2 * ceil_div(r, 16) * kParts * 1024; }
 
 // ---- expand ------------------------------------------------------------------------------------------------------------------
 // A wavefront computes up to 64 rows of 16 NJ columns, 16 rows at a time.  The MFMA's first operand is P, its second M_a; accumulator j of
@@ -526,7 +528,7 @@ __device__ __forceinline__ void copy_rows(const void* y_in, void* y_out, int N, 
 constexpr int kExpandCols = kExpandWaves * 16;  // of a workgroup, times NJ
 
 // FROM_SUMS: the workgroup adds v's slices and splits it itself, into s_p (as launch_shrink left them, [slices][T][r]).
-template <typename YT, int SPLIT, int CH, int NJ, bool FROM_SUMS = false>
+template <typename YT, int CH, int NJ, bool FROM_SUMS = false>
 __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int which, int32_t* s_rows, char* s_buf, u32x4* s_p = nullptr) {
   constexpr int BYTES = NJ * (int)sizeof(YT) < 16 ? NJ * (int)sizeof(YT) : 16, W = BYTES / (int)sizeof(YT), UNITS = NJ / W;
   constexpr int COLS = 16 * NJ, U = kTileRows / 16;
@@ -554,18 +556,18 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
   YT* out = static_cast<YT*>(e.y_out);
   const int c0 = nbase + ln * W;
   unit y[2][4][UNITS];
-  u32x4 p[2][CH][SPLIT];
+  u32x4 p[2][CH][kParts];
   // (no load under a condition: the compiler would wait for all loads behind it)
   const unit* const base = in != nullptr ? reinterpret_cast<const unit*>(in) : reinterpret_cast<const unit*>(e.m);
   const int in_last = in != nullptr ? e.N - W : 0;
   const size_t in_stride = in != nullptr ? e.N : 0;
-  const auto load = [&](unit(&yy)[4][UNITS], u32x4(&pp)[CH][SPLIT], int u) {
+  const auto load = [&](unit(&yy)[4][UNITS], u32x4(&pp)[CH][kParts], int u) {
     if constexpr (!FROM_SUMS) {
-      const u32x4* const from = e.packed + ((size_t)tile.at * U + u) * chunks * SPLIT * 64 + lane;
+      const u32x4* const from = e.packed + ((size_t)tile.at * U + u) * chunks * kParts * 64 + lane;
 #pragma unroll
       for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int s = 0; s < SPLIT; ++s) pp[c][s] = from[(min(c, chunks - 1) * SPLIT + s) * 64];
+        for (int s = 0; s < kParts; ++s) pp[c][s] = from[(min(c, chunks - 1) * kParts + s) * 64];
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -627,8 +629,8 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
         for (int k = 0; k < 8; ++k) v[k] *= scale;
       }
 #pragma unroll
-      for (int s = 0; s < SPLIT; ++s)
-        s_p[((row / 16 * CH + j0 / 32) * SPLIT + s) * 64 + j0 % 32 / 8 * 16 + row % 16] = take_bf16(v);
+      for (int s = 0; s < kParts; ++s)
+        s_p[((row / 16 * CH + j0 / 32) * kParts + s) * 64 + j0 % 32 / 8 * 16 + row % 16] = take_bf16(v);
     }
     __syncthreads();
     if (nbase >= e.N) return;
@@ -659,8 +661,8 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int s = SPLIT - 1; s >= 0; --s) {  // the small parts first
-        const u32x4 a = FROM_SUMS ? s_p[((u * CH + c) * SPLIT + s) * 64 + lane] : p[u & 1][c][s];
+      for (int s = kParts - 1; s >= 0; --s) {  // the small parts first
+        const u32x4 a = FROM_SUMS ? s_p[((u * CH + c) * kParts + s) * 64 + lane] : p[u & 1][c][s];
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[j] = mfma(a, w[c][j], acc[j]);
       }
@@ -683,19 +685,19 @@ __device__ __forceinline__ void expand_tile(const Expand& e, int col_block, int 
   }
 }
 
-template <typename YT, int SPLIT, int CH, int NJ, bool FROM_SUMS>
+template <typename YT, int CH, int NJ, bool FROM_SUMS>
 __global__ __launch_bounds__(kExpandThreads, 2) void expand_kernel(Expand e, int n_tiles) {
   __shared__ int32_t s_rows[kTileRows];
-  __shared__ u32x4 s_p[FROM_SUMS ? kTileRows / 16 * CH * SPLIT * 64 : 1];
+  __shared__ u32x4 s_p[FROM_SUMS ? kTileRows / 16 * CH * kParts * 64 : 1];
   __shared__ __align__(16) char s_buf[kExpandCols * NJ * 64];
   const int which = blockIdx.z * gridDim.y + blockIdx.y;
-  if (which < n_tiles) expand_tile<YT, SPLIT, CH, NJ, FROM_SUMS>(e, blockIdx.x, which, s_rows, s_buf, s_p);
+  if (which < n_tiles) expand_tile<YT, CH, NJ, FROM_SUMS>(e, blockIdx.x, which, s_rows, s_buf, s_p);
 }
 
-template <typename YT, int SPLIT, int CH, int NJ, bool FROM_SUMS>
+template <typename YT, int CH, int NJ, bool FROM_SUMS>
 void launch_expand_kernel(const Expand& e, int n_tiles, hipStream_t s) {
   constexpr int kMaxY = 32768;  // (a grid's y is 16 bits)
-  hipLaunchKernelGGL((expand_kernel<YT, SPLIT, CH, NJ, FROM_SUMS>),
+  hipLaunchKernelGGL((expand_kernel<YT, CH, NJ, FROM_SUMS>),
                      dim3(ceil_div(e.N, kExpandCols * NJ), n_tiles < kMaxY ? n_tiles : kMaxY, ceil_div(n_tiles, kMaxY)),
                      dim3(kExpandThreads), 0, s, e, n_tiles);
 }
@@ -705,8 +707,6 @@ void launch_expand_kernel(const Expand& e, int n_tiles, hipStream_t s) {
 // either; of the nine products of parts the three below 2^-23 of the whole are left out, so that the sums are as exact as fp32 products'.
 // A wavefront has 64 columns of all 64 rows in its accumulators and takes 32 of M's columns after the other, the next ones on their way
 // meanwhile.  P's parts lie in LDS, where the workgroup's four wavefronts share them.
-constexpr int kParts = 3;
-
 struct ExpandF32 {
   int T;
   const u32x4* packed;   // [tiles][4][chunks of 32 columns][kParts][64]
@@ -802,7 +802,7 @@ __device__ __forceinline__ void expand_f32_tile(const ExpandF32& e, int col_bloc
 // ---- outer -------------------------------------------------------------------------------------------------------------------
 // A wavefront takes 32 rows at a time: lane (c, q) loads 8 neighbouring columns of rows 8 q .. 8 q + 7, a row's 16 lanes 256 bytes in a
 // row, and byte permutations turn the eight 16-byte rows into eight column fragments (rows are the sum's index): no trip through
-// LDS.  P's fragments come packed in three parts.  The wavefronts take every fourth 32 rows; their sums are added in order through LDS,
+// LDS.  P's fragments come packed in parts.  The wavefronts take every fourth 32 rows; their sums are added in order through LDS,
 // one tile of P's columns at a time.  A group of more than `chunk` rows is cut, its pieces' sums go to `part` and join in
 // reduce_kernel: which pieces there are follows from the rows alone, so the order of the additions is fixed.  8192 rows of 4096 and 4096
 // columns at rank 64: 50 us, 27 without P, whose fragments each column tile reads from L2 anew (200 MB beside 134 MB of Z).
@@ -852,10 +852,10 @@ __device__ __forceinline__ void outer_tile(const Outer& o, int tile_of_cols, int
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const uint16_t* const zc = sd.z + min(c0 + 8 * c, sd.cols - 8);  // columns past the end are computed and not stored
   const int blocks = (tile.rows + 31) / 32;
-  const u32x4* const packed = sd.packed + ((size_t)tile.at * tiles + m0) * 3 * 64 + lane;
+  const u32x4* const packed = sd.packed + ((size_t)tile.at * tiles + m0) * kParts * 64 + lane;
   const int m_last = min(MT, tiles - m0) - 1;  // (tiles past the last: computed from it again and not stored)
   constexpr int FIRST = MT < 2 ? MT : 2;  // tiles of P's columns whose parts are loaded a block ahead
-  u32x4 z[8], p[FIRST][3];
+  u32x4 z[8], p[FIRST][kParts];
   const auto load_z = [&](int b) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -863,9 +863,9 @@ __device__ __forceinline__ void outer_tile(const Outer& o, int tile_of_cols, int
       z[i] = *reinterpret_cast<const u32x4*>(zc + (size_t)(o.list != nullptr ? s_rows[at] : tile.first + at) * sd.cols);
     }
   };
-  const auto load_p = [&](u32x4(&v)[3], int b, int m) {
+  const auto load_p = [&](u32x4(&v)[kParts], int b, int m) {
 #pragma unroll
-    for (int s = 0; s < 3; ++s) v[s] = packed[((size_t)b * tiles + min(m, m_last)) * 3 * 64 + s * 64];
+    for (int s = 0; s < kParts; ++s) v[s] = packed[((size_t)b * tiles + min(m, m_last)) * kParts * 64 + s * 64];
   };
   int b = wave;
   if (b < blocks) {
@@ -875,7 +875,7 @@ __device__ __forceinline__ void outer_tile(const Outer& o, int tile_of_cols, int
   }
   for (; b < blocks; b += kOuterWaves) {
     const int next = min(b + kOuterWaves, blocks - 1);
-    u32x4 f[8], late[MT > FIRST ? MT - FIRST : 1][3];
+    u32x4 f[8], late[MT > FIRST ? MT - FIRST : 1][kParts];
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
       uint32_t lo[4], hi[4];
@@ -894,7 +894,7 @@ __device__ __forceinline__ void outer_tile(const Outer& o, int tile_of_cols, int
 #pragma unroll
     for (int m = 0; m < FIRST; ++m)
 #pragma unroll
-      for (int s = 0; s < 3; ++s)
+      for (int s = 0; s < kParts; ++s)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[m][j] = mfma(p[m][s], f[j], acc[m][j]);
 #pragma unroll
@@ -904,7 +904,7 @@ __device__ __forceinline__ void outer_tile(const Outer& o, int tile_of_cols, int
 #pragma unroll
     for (int m = FIRST; m < MT; ++m)
 #pragma unroll
-      for (int s = 0; s < 3; ++s)
+      for (int s = 0; s < kParts; ++s)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[m][j] = mfma(late[m - FIRST][s], f[j], acc[m][j]);
   }
@@ -975,7 +975,7 @@ struct ExpandByGroup {
   typedef Expand Args;
   static constexpr int kCols = kExpandCols * NJ, kBytes = kExpandCols * NJ * 64;
   static __device__ __forceinline__ void run(const Args& e, int col_block, int which, int32_t* s_rows, char* s_buf) {
-    expand_tile<uint16_t, 2, CH, NJ>(e, col_block, which, s_rows, s_buf);
+    expand_tile<uint16_t, CH, NJ>(e, col_block, which, s_rows, s_buf);
   }
 };
 struct ExpandByF32 {
