@@ -89,9 +89,9 @@ class Adapters(NamedTuple):
 
 class Gradients(NamedTuple):
     """What ExpertShardLayer.backward leaves: views of the layer's buffers, valid until its next call of it."""
-    dx: torch.Tensor | None              # [T,H] bf16
+    dx: torch.Tensor | None              # [T,H] bf16; None also where nothing here reads x (given logits, no gate, no ids, no dx_in)
     logits: torch.Tensor                 # [T,E] fp32
-    w_router: torch.Tensor | None        # [H,E] fp32
+    w_router: torch.Tensor | None        # [H,E] fp32; None after a forward of given logits, which does not read the weights
     w_shared_gate: torch.Tensor | None   # [H] fp32
     adapter_a: torch.Tensor | None       # [L][rank][H] fp32
     adapter_b: torch.Tensor | None       # [L][H][rank] fp32
@@ -176,6 +176,7 @@ class ExpertShardLayer:
         self._side = _side_stream(device) if self.overlap_shared else None
         self.Tmax, self._grad_tmax = -1, -1
         self._has_v = False   # the last forward kept the module's adapters' v
+        self._own_logits = False  # it computed the logits itself
         # {0, T} for the shared expert's call, one immutable device tensor per token count: a
         # captured graph keeps reading the tensor it was captured with
         self._sh_offsets = {}
@@ -388,6 +389,7 @@ class ExpertShardLayer:
                 raise RuntimeError("run one eager forward with this token count before capturing a graph")
             self._alloc(T)
         self._last_T, self._has_v = T, adapter_idx is not None and self.adapters is not None
+        self._own_logits = logits is None
         k, H = self.k, self.H
         plan = self._plan(T)
         # the FFN scratch depends on the regime (decode-sized calls need split-K partials)
@@ -485,8 +487,9 @@ class ExpertShardLayer:
                  token_mask: torch.Tensor | None = None, coef_balance: float = 0.0, coef_z: float = 0.0,
                  dx_in: torch.Tensor | None = None, need_dx: bool = True, stream=None) -> Gradients:
         """Gradients of the last forward, of the same x and adapter_idx, for dy [T,H] bf16 and the router's losses times their
-        coefficients.  The experts' own weights are frozen.  dx holds what reaches x through the router, the shared expert's
-        gate and the module's adapters, added to dx_in, the part through the experts.  A shard's gradients are its part of a
+        coefficients.  The experts' own weights are frozen.  dx holds what reaches x through the router (not after given logits,
+        whose gradient is Gradients.logits), the shared expert's gate and the module's adapters, added to dx_in, the part through the
+        experts, which the caller brings: nothing here computes it.  A shard's gradients are its part of a
         sum: those of all shards, the losses' coefficients given to one of them, add up to the unsharded layer's."""
         T, H, E = self._rows(), self.H, self.E
         if token_mask is not None:
@@ -516,7 +519,8 @@ class ExpertShardLayer:
         B.moe_route_backward(self.logits, self.topk_idx, self.d_topk_w, token_mask, self.counts if losses else None, T, E, self.k,
                              coef_balance, coef_z, B.MOE_RENORM_TOPK if self.renorm else 0, self.d_logits, stream)
         dx = self.dx if need_dx else None
-        if self.w_router is not None:
+        router = self.w_router is not None and self._own_logits
+        if router:
             B.moe_router_backward(x, self.w_router, self.d_logits, T, H, E, dx_in, dx, self.d_w_router, self.grad_ws, stream)
             dx_in = dx
         if gate:
@@ -530,7 +534,7 @@ class ExpertShardLayer:
             dx_in = dx
         if need_dx and dx_in is not dx:   # logits from outside and nothing else that reads x
             dx = dx_in
-        return Gradients(None if dx is None else dx[:T], self.d_logits[:T], self.d_w_router if self.w_router is not None else None,
+        return Gradients(None if dx is None else dx[:T], self.d_logits[:T], self.d_w_router if router else None,
                          self.d_w_shared_gate[:, 0] if gate else None, self.grad_a if adapter_idx is not None else None,
                          self.grad_b if adapter_idx is not None else None)
 
