@@ -384,8 +384,10 @@ class ExpertShardLayer:
             if self.adapters is None and self.shared_adapters is None:
                 raise ValueError("adapter_idx for a layer without adapters")
             self._check_rows(adapter_idx, "adapter_idx", (T,), torch.int32)
+        capturing = torch.cuda.is_current_stream_capturing()
+        self._captured |= capturing      # by capture() or by the caller
         if T > self.Tmax:
-            if torch.cuda.is_current_stream_capturing():
+            if capturing:
                 raise RuntimeError("run one eager forward with this token count before capturing a graph")
             self._alloc(T)
         self._last_T, self._has_v = T, adapter_idx is not None and self.adapters is not None
@@ -399,6 +401,11 @@ class ExpertShardLayer:
         if self.shared is not None and plan.ffn_ws_sh > self.ffn_ws_sh.numel():
             self._retire(("ffn_ws_sh",))
             self.ffn_ws_sh = torch.empty(plan.ffn_ws_sh, dtype=torch.uint8, device=self.device)
+        if adapter_idx is not None and self._lora_bytes(T) > self.lora_ws.numel():
+            if capturing:
+                raise RuntimeError("run one eager forward with this token count before capturing a graph")
+            self._retire(("lora_ws",))
+            self.lora_ws = torch.empty(self._lora_bytes(T), dtype=torch.uint8, device=self.device)
         flags = B.MOE_RENORM_TOPK if self.renorm else 0
         if logits is not None:
             self.logits[:T].copy_(logits)
@@ -415,9 +422,6 @@ class ExpertShardLayer:
             ptr(self.workspace), self.workspace.numel(), ptr(self.w_gate), ptr(self.w_up), ptr(self.w_down),
             ptr(self.h_ws), ptr(self.y_perm), ptr(self.ffn_ws), self.ffn_ws.numel(),
             None, ptr(gate_x), ptr(self.w_shared_gate), ptr(self.y_out), T, k, flags, yflag | plan.hint, cflags)
-        if adapter_idx is not None and self._lora_bytes(T) > self.lora_ws.numel():
-            self._retire(("lora_ws",))
-            self.lora_ws = torch.empty(self._lora_bytes(T), dtype=torch.uint8, device=self.device)
         if self.shared is None:
             B.moe_forward(args, self.shard, self.ffn_shard, stream)
             self._add_adapters(x, adapter_idx, T, stream)
@@ -440,7 +444,7 @@ class ExpertShardLayer:
             # Eager, the shared expert first: it starts while the host enqueues the others.  A graph runs its branches in the
             # order of their first kernels and the combine on the first one's queue, so there the routed experts, where they
             # end last, come first: a queue waits 10 us for another one's kernel.
-            if torch.cuda.is_current_stream_capturing() and plan.routed_first:
+            if capturing and plan.routed_first:
                 B.moe_forward(args, self.shard, self.ffn_shard, main)
                 shared()
             else:
@@ -548,7 +552,6 @@ class ExpertShardLayer:
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         graph = torch.cuda.CUDAGraph()
-        self._captured = True
         with torch.cuda.stream(side):
             with torch.cuda.graph(graph, stream=side):
                 out = self.forward(x, logits, adapter_idx=adapter_idx)

@@ -42,3 +42,29 @@ def test_dx_after_given_logits_where_nothing_else_reads_x():
     assert layer.backward(x, dy).dx is None
     more = torch.randn(20, H, device="cuda").bfloat16()
     assert torch.equal(layer.backward(x, dy, dx_in=more).dx, more)
+
+
+@pytest.mark.parametrize("T", [16, 200])
+def test_a_forward_captured_alone_keeps_its_buffers(T):
+    """Captured with torch.cuda.graph, not by layer.capture: a larger eager batch takes none of the graph's buffers away."""
+    w = _weights()
+    x, _, idx, _ = _batch(T)
+    layer, eager = _layer(w), _layer(w)
+    layer.forward(x, adapter_idx=idx)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = layer.forward(x, adapter_idx=idx)
+    kept = {n: getattr(layer, n) for n in layer._BUFFERS if getattr(layer, n, None) is not None}
+    big = _batch(T + 500)
+    layer.forward(big[0], adapter_idx=big[2])
+    for name, buffer in kept.items():
+        assert getattr(layer, name) is buffer or any(buffer is r for r in layer._retired), name
+    filler = [torch.full((1 << 20,), 1.0, device="cuda") for _ in range(8)]
+    for seed in (1, 2, 3):
+        new = _batch(T, seed)
+        x.copy_(new[0]), idx.copy_(new[2])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager.forward(x, adapter_idx=idx))
+    assert all(bool((f == 1).all()) for f in filler)
