@@ -134,7 +134,8 @@ class ExpertShardLayer:
     ``adapter_idx`` names for token t (outside 0 .. L-1: none); ``shared_adapters`` are those of the shared expert's down
     projection, which read its activated rows.  Shards' outputs add up with them too: the module's belong to one shard, or
     each shard holds some of their ranks; the down projection's are sliced along K as w_down is.
-    ``backward`` trains what is not frozen beside the experts: the router, the shared expert's gate and the module's adapters.
+    ``backward`` trains what is not frozen beside the experts: the router, the shared expert's gate and the module's adapters (not
+    ``shared_adapters``).
     """
 
     def __init__(self, *, n_experts, top_k, hidden, inter_full, inter_slice, n_local_experts=None, expert_offset=0,
@@ -491,10 +492,11 @@ class ExpertShardLayer:
                  token_mask: torch.Tensor | None = None, coef_balance: float = 0.0, coef_z: float = 0.0,
                  dx_in: torch.Tensor | None = None, need_dx: bool = True, stream=None) -> Gradients:
         """Gradients of the last forward, of the same x and adapter_idx, for dy [T,H] bf16 and the router's losses times their
-        coefficients.  The experts' own weights are frozen.  dx holds what reaches x through the router (not after given logits,
+        coefficients.  The experts' own weights are frozen, and so are the shared_adapters.  dx holds what reaches x through the router (not after given logits,
         whose gradient is Gradients.logits), the shared expert's gate and the module's adapters, added to dx_in, the part through the
-        experts, which the caller brings: nothing here computes it.  A shard's gradients are its part of a
-        sum: those of all shards, the losses' coefficients given to one of them, add up to the unsharded layer's."""
+        experts, which the caller brings: nothing here computes it.  After a forward with adapter_idx a call without needs
+        need_dx=False: the router and the gate alone are trained then.  A shard's gradients are its part of a sum: those of all
+        shards, the losses' coefficients given to one of them, add up to the unsharded layer's."""
         T, H, E = self._rows(), self.H, self.E
         if token_mask is not None:
             self._check_rows(token_mask, "token_mask", (T,), torch.uint8)
@@ -503,15 +505,16 @@ class ExpertShardLayer:
         if adapter_idx is not None:
             if self.adapters is None:
                 raise ValueError("adapter_idx for a layer without adapters")
-            if self.shared_adapters is not None:
-                raise ValueError("the adapters of the shared expert's down projection are served, not trained")
             if not self._has_v:
                 raise ValueError("adapter_idx for a forward without")
             self._check_rows(adapter_idx, "adapter_idx", (T,), torch.int32)
+        elif self._has_v and need_dx:
+            raise ValueError("the forward had adapter_idx, which dx needs (need_dx=False trains the router and the gate alone)")
         if dx_in is not None:
             self._check_rows(dx_in, "dx_in", (T, H), torch.bfloat16)
             if not need_dx:
                 raise ValueError("dx_in without dx")
+        B._ptrs(x, dy, adapter_idx, token_mask, dx_in)   # on this device and contiguous, before anything is launched
         self._room_for_grad(T)
         gate = self.w_shared_gate is not None and self.shared is not None
         B.moe_combine_backward(dy, self.y_perm, self.slot_row, T, self.k, H, self.y_shared if gate else None, x if gate else None,

@@ -68,3 +68,20 @@ def test_a_forward_captured_alone_keeps_its_buffers(T):
         torch.cuda.synchronize()
         assert torch.equal(out, eager.forward(x, adapter_idx=idx))
     assert all(bool((f == 1).all()) for f in filler)
+
+
+@pytest.mark.parametrize("T", [9, 200])
+def test_the_modules_adapters_are_trained_beside_frozen_ones(T):
+    """A layer that serves adapters of the shared expert's down projection too: all gradients but those, from the same ids."""
+    w = _weights()
+    x, dy, idx, mask = _batch(T)
+    mask[0] = 1
+    layer = _layer(w, down=True)
+    layer.forward(x, adapter_idx=idx)
+    with pytest.raises(ValueError):
+        layer.backward(x, dy)                        # dx without the module's adapters would lack a part
+    got = layer.backward(x, dy, idx, mask, 0.5, 0.25)
+    ref, _, _ = _chain(layer, w, x, dy, idx, mask, 0.5, 0.25, True, True)
+    _compare(got, ref, list(ref))
+    only = layer.backward(x, dy, None, mask, need_dx=False)
+    assert only.dx is None and only.adapter_a is None and only.w_router is not None
