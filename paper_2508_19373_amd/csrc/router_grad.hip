@@ -485,8 +485,8 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const uint16
     float sum = 0.f, logit = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) sum += red[w][KMAX], logit += red[w][KMAX + 1];
-    const float gate = 1.f / (1.f + expf(-logit));
-    d_shared_gate[t] = gate * (1.f - gate) * sum;
+    const float e = expf(-fabsf(logit));  // gate (1 - gate) without a difference: both ends keep their digits
+    d_shared_gate[t] = e / ((1.f + e) * (1.f + e)) * sum;
   }
 }
 

@@ -1,0 +1,32 @@
+"""The router's gradients where a formula that is right on paper loses its digits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2508_19373_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_shared_gate_far_from_its_middle(sign, bf16):
+    """The gate's logits are 8 to 60 on one side.  g (1 - g) follows its logit z with a relative slope of 1 at most: the relative error is
+    that of z, a sum of H products of one sign, (H + 8) 2^-23 |z|, that of the products with y_shared, (H + 8) 2^-23 of their absolute
+    sum, and 2^-20 for the exponential and what is made of it."""
+    T, H, k = 53, 64, 2
+    g = torch.Generator().manual_seed(4)
+    dt = torch.bfloat16 if bf16 else torch.float32
+    x = (torch.rand((T, H), generator=g) + 0.5).bfloat16()
+    w = torch.rand(H, generator=g) + 0.5
+    z = torch.linspace(8.0, 60.0, T).double()
+    x = (x.double() * (z / (x.double() @ w.double()))[:, None] * sign).bfloat16()
+    dy, ys, y = torch.randn((T, H), generator=g).bfloat16(), torch.randn((T, H), generator=g).to(dt), torch.zeros((T * k, H), dtype=dt)
+    d = [t.cuda() for t in (dy, y, torch.arange(T * k, dtype=torch.int32), ys, x, w)]
+    dw, dg = torch.empty((T, k), device="cuda"), torch.empty(T, device="cuda")
+    B.moe_combine_backward(d[0], d[1], d[2], T, k, H, *d[3:], dw, dg, B.MOE_Y_PERM_BF16 if bf16 else 0)
+    z = (x.double() @ w.double()).numpy()
+    slope = np.exp(-np.abs(z)) / (1 + np.exp(-np.abs(z))) ** 2
+    terms = (dy.double() * ys.double()).numpy()
+    bound = slope * np.abs(terms).sum(1) * ((H + 8) * 2.0 ** -23 * (1 + np.abs(z)) + 2.0 ** -20)
+    assert (np.abs(dg.double().cpu().numpy() - slope * terms.sum(1)) <= bound).all()
