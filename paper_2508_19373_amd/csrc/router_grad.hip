@@ -58,20 +58,10 @@ __device__ __forceinline__ void group_sum(float (&v)[U]) {
   group_reduce<G, U>(v, [](float a, float b) { return a + b; });
 }
 
-// 1 / v to the last place or so: the hardware's estimate and one step.
-__device__ __forceinline__ float reciprocal(float v) {
-#ifdef __HIP_DEVICE_COMPILE__
-  const float r = __builtin_amdgcn_rcpf(v);
-  return fmaf(fmaf(-v, r, 1.f), r, r);
-#else
-  return 1.f / v;
-#endif
-}
-
-// p: the tokens' logits on entry, their softmax on return (0 past E); lse: log sum exp.
+// p: the tokens' logits on entry, exp(logit - the largest) on return (0 past E), whose sum is `sum`; lse: log sum exp.
 template <int G, int S, int U>
-__device__ __forceinline__ void group_softmax(float (&p)[U][S], int l, int E, float (&lse)[U]) {
-  float top[U], sum[U];
+__device__ __forceinline__ void group_softmax(float (&p)[U][S], int l, int E, float (&sum)[U], float (&lse)[U]) {
+  float top[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     top[u] = -INFINITY;
@@ -90,12 +80,7 @@ __device__ __forceinline__ void group_softmax(float (&p)[U][S], int l, int E, fl
   }
   group_sum<G, U>(sum);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const float inv = reciprocal(sum[u]);
-#pragma unroll
-    for (int s = 0; s < S; ++s) p[u][s] *= inv;
-    lse[u] = top[u] + logf(sum[u]);
-  }
+  for (int u = 0; u < U; ++u) lse[u] = top[u] + logf(sum[u]);
 }
 
 // ---- balance loss ----------------------------------------------------------------------------------------------------------
@@ -157,7 +142,7 @@ __global__ __launch_bounds__(kLossThreads) void balance_kernel(Balance b) {
   const uint8_t* const mask = b.mask != nullptr ? b.mask : reinterpret_cast<const uint8_t*>(b.logits);
   const int step = gridDim.x * kGroups;
   for (int t0 = blockIdx.x * kGroups + group; t0 < b.T; t0 += U * step) {
-    float p[U][S], lse[U];
+    float p[U][S], all[U], lse[U];
     int e[U][PICKED];
     bool in[U];
 #pragma unroll
@@ -169,7 +154,7 @@ __global__ __launch_bounds__(kLossThreads) void balance_kernel(Balance b) {
 #pragma unroll
       for (int i = 0; i < PICKED; ++i) e[u][i] = b.idx[(size_t)t * b.k + min(l + G * i, b.k - 1)];
     }
-    group_softmax<G, S, U>(p, l, E, lse);
+    group_softmax<G, S, U>(p, l, E, all, lse);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (!in[u] || t0 + u * step >= b.T) continue;
@@ -179,7 +164,7 @@ __global__ __launch_bounds__(kLossThreads) void balance_kernel(Balance b) {
       if (l == 0) atomicAdd(&cnt[E], 1);
       z = fmaf(lse[u], lse[u], z);
 #pragma unroll
-      for (int s = 0; s < S; ++s) mine[s] += p[u][s];
+      for (int s = 0; s < S; ++s) mine[s] += p[u][s] / all[u];
     }
   }
 #pragma unroll
@@ -263,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward 
   const bool gates = b.d_topk_w != nullptr, losses = b.counts != nullptr;
   const uint8_t* const mask = b.mask != nullptr ? b.mask : reinterpret_cast<const uint8_t*>(b.logits);
   const float* const d_topk_w = gates ? b.d_topk_w : b.logits;
-  float p[U][S], lse[U], load[S], grads[U][PICKED];
+  float p[U][S], all[U], lse[U], load[S], grads[U][PICKED];
   int ids[U][PICKED];
   bool counted[U];
 #pragma unroll
@@ -302,41 +287,48 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward 
         if (l + G * i < k && (unsigned)ids[u][i] < (unsigned)E) s_picked[group][u][ids[u][i]] = make_float2(1.f, grads[u][i]);
     wave_fence();
   }
-  group_softmax<G, S, U>(p, l, E, lse);
-  float f[U][S], gate_dot[U], gate_sum[U], dot[U];
+  group_softmax<G, S, U>(p, l, E, all, lse);
+  float f[U][S], w[U][S], gate_dot[U], gate_sum[U], dot[U];  // w: the picked experts' own softmax
+  const bool renormed = b.renorm && gates;
+  if (renormed) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      gate_sum[u] = 0.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        w[u][s] = s_picked[group][u][l + G * s].x * p[u][s];
+        gate_sum[u] += w[u][s];
+      }
+    }
+    group_sum<G, U>(gate_sum);
+  }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    gate_dot[u] = gate_sum[u] = dot[u] = 0.f;
+    gate_dot[u] = dot[u] = 0.f;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      const float2 v = gates ? s_picked[group][u][l + G * s] : make_float2(0.f, 0.f);
+      const float grad = gates ? s_picked[group][u][l + G * s].y : 0.f;
+      p[u][s] /= all[u];
       f[u][s] = counted[u] ? load[s] : 0.f;
-      if (b.renorm) {
-        gate_sum[u] = fmaf(v.x, p[u][s], gate_sum[u]);
-        gate_dot[u] = fmaf(v.y, p[u][s], gate_dot[u]);
+      if (renormed) {
+        w[u][s] /= gate_sum[u] > 0.f ? gate_sum[u] : 1.f;  // (1 exactly where one expert is picked: its gradient is 0)
+        gate_dot[u] = fmaf(grad, w[u][s], gate_dot[u]);
       } else {
-        f[u][s] += v.y;
+        f[u][s] += grad;
       }
       dot[u] = fmaf(p[u][s], f[u][s], dot[u]);
     }
   }
   group_sum<G, U>(dot);
-  if (b.renorm && gates) {
-    group_sum<G, U>(gate_sum);
-    group_sum<G, U>(gate_dot);
-  }
+  if (renormed) group_sum<G, U>(gate_dot);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (t0 + u >= b.T) break;
     const float z = counted[u] ? cz * lse[u] : 0.f;
-    const float inv = b.renorm && gates ? reciprocal(gate_sum[u]) : 0.f, mean = gate_dot[u] * inv;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       float d = counted[u] || (gates && !b.renorm) ? p[u][s] * (f[u][s] - dot[u] + z) : 0.f;
-      if (b.renorm && gates) {
-        const float2 v = s_picked[group][u][l + G * s];
-        if (v.x != 0.f) d = fmaf(p[u][s] * inv, v.y - mean, d);
-      }
+      if (renormed) d = fmaf(w[u][s], s_picked[group][u][l + G * s].y - gate_dot[u], d);
       if (l + G * s < E) b.d_logits[(size_t)(t0 + u) * E + l + G * s] = d;
     }
   }

@@ -30,3 +30,14 @@ def test_shared_gate_far_from_its_middle(sign, bf16):
     terms = (dy.double() * ys.double()).numpy()
     bound = slope * np.abs(terms).sum(1) * ((H + 8) * 2.0 ** -23 * (1 + np.abs(z)) + 2.0 ** -20)
     assert (np.abs(dg.double().cpu().numpy() - slope * terms.sum(1)) <= bound).all()
+
+
+@pytest.mark.parametrize("T,E", [(1, 1), (70, 8), (300, 16), (65, 33), (200, 60), (3000, 64), (40, 130), (33, 256)])
+def test_one_renormalised_gate_has_no_gradient(T, E):
+    """A gate that is divided by itself is 1 whatever the logits are: its gradient is 0, not the last places of the one it is given."""
+    g = torch.Generator().manual_seed(T + E)
+    logits, dw = (torch.randn((T, E), generator=g) * 3).cuda(), (torch.randn((T, 1), generator=g) * 100).cuda()
+    idx = logits.argmax(1, keepdim=True).int()
+    d = torch.full((T, E), float("nan"), device="cuda")
+    B.moe_route_backward(logits, idx, dw, None, None, T, E, 1, 0.0, 0.0, B.MOE_RENORM_TOPK, d)
+    assert not d.any()
