@@ -501,7 +501,7 @@ Plan make_plan(int T, int K, int N, int rank, int L, bool backward) {
   p.offsets = take((L + 2) * sizeof(int32_t));
   p.list = take((size_t)T * sizeof(int32_t));
   p.tiles = take(p.n_tiles * sizeof(Tile));
-  p.packed = take(packed_bytes(p.n_tiles, rank));
+  p.packed = take(backward || !from_sums(T, rank, p.slices) ? packed_bytes(p.n_tiles, rank) : 0);
   if (backward) {
     p.chunk = outer_chunk(T, L, ceil_div(K, kOuterCols) + ceil_div(N, kOuterCols), rank, 512);
     p.n_pieces = T / p.chunk + L;
