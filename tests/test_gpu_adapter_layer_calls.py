@@ -85,3 +85,16 @@ def test_the_modules_adapters_are_trained_beside_frozen_ones(T):
     _compare(got, ref, list(ref))
     only = layer.backward(x, dy, None, mask, need_dx=False)
     assert only.dx is None and only.adapter_a is None and only.w_router is not None
+
+
+@pytest.mark.parametrize("overlap", [True, False])
+@pytest.mark.parametrize("T", [5, 150])
+def test_sliced_down_projections_adapters_add_up(T, overlap):
+    """Two tensor-parallel shards: their columns of the down projection's A (112 of 224, padded to 128), whole B; half of the module's ranks."""
+    w = _weights()
+    x, _, idx, _ = _batch(T)
+    want = _layer(w, down=True, out_f32=True, overlap_shared=overlap).forward(x, adapter_idx=idx).clone()
+    without = _layer(w, out_f32=True, overlap_shared=overlap).forward(x, adapter_idx=idx)
+    assert not torch.equal(without, want)
+    total = sum(_layer(w, down=True, tp=2, p=p, out_f32=True, overlap_shared=overlap).forward(x, adapter_idx=idx).clone() for p in range(2))
+    assert _rel(total, want) <= 1e-4        # as test_shards_add_up

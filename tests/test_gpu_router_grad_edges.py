@@ -41,3 +41,27 @@ def test_one_renormalised_gate_has_no_gradient(T, E):
     d = torch.full((T, E), float("nan"), device="cuda")
     B.moe_route_backward(logits, idx, dw, None, None, T, E, 1, 0.0, 0.0, B.MOE_RENORM_TOPK, d)
     assert not d.any()
+
+
+@pytest.mark.parametrize("T,E,k", [(130, 8, 2), (2000, 60, 4), (90, 200, 8)])
+def test_data_parallel_devices_sum_their_counts(T, E, k):
+    """Two devices' batches with the sums of their counts: row by row the gradients of the whole batch, bit for bit."""
+    g = torch.Generator().manual_seed(T)
+    logits, dw = torch.randn((T, E), generator=g).cuda(), torch.randn((T, k), generator=g).cuda()
+    idx, mask = logits.topk(k, dim=1).indices.int().contiguous(), (torch.rand(T, generator=g) < 0.7).to(torch.uint8).cuda()
+    ws = torch.empty(B.moe_balance_workspace_bytes(T, E), dtype=torch.uint8, device="cuda")
+
+    def counted(rows):
+        counts, prob, losses = torch.empty(E + 1, dtype=torch.int32, device="cuda"), torch.empty(E, device="cuda"), torch.empty(2, device="cuda")
+        B.moe_balance_loss(logits[rows], idx[rows], mask[rows], rows.stop - rows.start, E, k, counts, prob, losses, ws)
+        return counts
+
+    def gradient(rows, counts):
+        d = torch.full((rows.stop - rows.start, E), float("nan"), device="cuda")
+        B.moe_route_backward(logits[rows], idx[rows], dw[rows], mask[rows], counts, rows.stop - rows.start, E, k, 0.5, 0.25, 0, d)
+        return d
+    cut = T // 3
+    parts, whole = [slice(0, cut), slice(cut, T)], slice(0, T)
+    total = counted(parts[0]) + counted(parts[1])
+    assert torch.equal(total, counted(whole)) and int(total[E]) == int(mask.sum())
+    assert torch.equal(torch.cat([gradient(p, total) for p in parts]), gradient(whole, total))
