@@ -875,7 +875,7 @@ __device__ __forceinline__ void outer_tile(const Outer& o, int tile_of_cols, int
   }
   for (; b < blocks; b += kOuterWaves) {
     const int next = min(b + kOuterWaves, blocks - 1);
-    u32x4 f[8], late[MT > FIRST ? MT - FIRST : 1][kParts];
+    u32x4 f[8];
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
       uint32_t lo[4], hi[4];
@@ -887,26 +887,18 @@ __device__ __forceinline__ void outer_tile(const Outer& o, int tile_of_cols, int
       f[2 * d] = u32x4{lo[0], lo[1], lo[2], lo[3]};
       f[2 * d + 1] = u32x4{hi[0], hi[1], hi[2], hi[3]};
     }
-    // loads return in the order they are issued in: P's for this block, P's for the next, Z's for the next
+    // P's columns 32 ahead, the next block's after this one's; Z's rows between them, as loads return in the order they are issued in
 #pragma unroll
-    for (int m = FIRST; m < MT; ++m) load_p(late[m - FIRST], b, m);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int m = 0; m < FIRST; ++m)
+    for (int m = 0; m < MT; ++m) {
 #pragma unroll
       for (int s = 0; s < kParts; ++s)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[m][j] = mfma(p[m][s], f[j], acc[m][j]);
-#pragma unroll
-    for (int m = 0; m < FIRST; ++m) load_p(p[m], next, m);
-    load_z(next);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int m = FIRST; m < MT; ++m)
-#pragma unroll
-      for (int s = 0; s < kParts; ++s)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[m][j] = mfma(late[m - FIRST][s], f[j], acc[m][j]);
+        for (int j = 0; j < 8; ++j) acc[m][j] = mfma(p[m % FIRST][s], f[j], acc[m][j]);
+      if (m > 0 && m + FIRST == MT) load_z(next);
+      load_p(p[m % FIRST], m + FIRST < MT ? b : next, (m + FIRST) % MT);
+      if (MT == FIRST && m + 1 == MT) load_z(next);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
   const int slot = o.pieces != nullptr ? o.slots[piece] : (o.T > o.chunk ? piece : -1);
   const float scale = sd.scale != nullptr ? sd.scale[tile.group] : 1.f;
