@@ -13,7 +13,7 @@
  * Conventions as in moe_shard.h: status codes (MOE_OK / MOE_ERR_*), validation on the host before any HIP call, no allocation, no
  * synchronisation, work enqueued on `stream`; all pointers are DEVICE pointers owned by the caller, 16-byte aligned (adapter_idx and
  * scale: 4-byte).  With T == 0 the buffers of T rows may be NULL.  Values must be finite, except in the rows of x, dy and v whose
- * request has no adapter: those are not used.
+ * request has no adapter, and in lora_a, lora_b and scale of an adapter that no row has: those are not used.
  * A call writes all of its workspace that it reads, so nothing has to start at zero; calls that overlap on one GPU (different
  * streams, graphs replayed concurrently) each bring their own.
  */

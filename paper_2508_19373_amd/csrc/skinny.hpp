@@ -901,7 +901,7 @@ __device__ __forceinline__ void outer_tile(const Outer& o, int tile_of_cols, int
     }
   }
   const int slot = o.pieces != nullptr ? o.slots[piece] : (o.T > o.chunk ? piece : -1);
-  const float scale = sd.scale != nullptr ? sd.scale[tile.group] : 1.f;
+  const float scale = sd.scale != nullptr && tile.rows > 0 ? sd.scale[tile.group] : 1.f;  // (without rows: zeros, whatever the scale is)
   float* out = slot >= 0 ? sd.part + (size_t)slot * r * sd.cols : sd.out + (size_t)tile.group * r * sd.cols;
 #pragma unroll
   for (int m = 0; m < MT; ++m) {

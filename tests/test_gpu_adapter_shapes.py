@@ -103,3 +103,27 @@ def test_groups_cut_into_long_pieces(K, N, r, counts):
     d = {n: t.cuda() if torch.is_tensor(t) else t for n, t in host.items()}
     v = torch.from_numpy(np.random.default_rng(T).standard_normal((T, r))).float().cuda()
     _backward(d, v)
+
+
+@pytest.mark.parametrize("T,K,N,r", [(6, 520, 264, 16), (48, 4096, 264, 64), (150, 136, 264, 16), (700, 1032, 520, 72), (9000, 136, 72, 8)])
+def test_slots_without_an_adapter_may_hold_anything(T, K, N, r):
+    """Of five slots three are in use; what lies in the others, NaN here, reaches nothing, and their gradients are zeros."""
+    L = 5
+    host = _make(T, T, K, N, r, L, "one")
+    host["idx"] = torch.tensor([1, 3, 2])[torch.arange(T) % 3].int()
+    d = {n: t.cuda() if torch.is_tensor(t) else t for n, t in host.items()}
+    clean = {n: t.clone() if torch.is_tensor(t) else t for n, t in d.items()}
+    for n in ("a", "b", "scale"):
+        d[n][0] = d[n][4] = float("nan")
+
+    def step(one):
+        y, v = torch.empty((T, N), device="cuda"), torch.empty((T, r), device="cuda")
+        dx, ga, gb = torch.empty_like(one["x"]), torch.empty((L, r, K), device="cuda"), torch.empty((L, N, r), device="cuda")
+        ws = torch.empty(max(B.moe_lora_workspace_bytes(T, K, N, r, L, back) for back in (False, True)), dtype=torch.uint8, device="cuda")
+        B.moe_lora_forward(one["x"], one["idx"], T, K, N, r, L, one["a"], one["b"], one["scale"], None, y, v, ws, B.MOE_OUT_F32)
+        B.moe_lora_backward(one["x"], one["dy"], one["idx"], T, K, N, r, L, one["a"], one["b"], one["scale"], v, None, dx, ga, gb, ws)
+        return y, v, dx, ga, gb
+    got, want = step(d), step(clean)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert not any(t[i].any() for t in got[3:] for i in (0, 4))
