@@ -403,7 +403,7 @@ struct RouterPlan {
 };
 RouterPlan plan_router(int T, int H, int E) {
   RouterPlan p = {};
-  p.chunk = outer_chunk(T, 1, ceil_div(H, kOuterCols), E, 128);
+  p.chunk = outer_chunk(T, 1, ceil_div(H, kOuterCols), E, 256);
   p.pieces = T > p.chunk ? ceil_div(T, p.chunk) : 1;
   p.slots = T > p.chunk ? p.pieces : 0;
   p.tiles = ceil_div(T, kTileRows);

@@ -1053,16 +1053,12 @@ inline void launch_reduce(const Outer& o, hipStream_t s) {
   hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div(values, 1024), o.L), dim3(256), 0, s, o);
 }
 
-// Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.  The router wants 128, beside which dx's
-// workgroups, two to four times as many, fill the units, and has fewer parts to join (256 / 128 / 512, us: 2048 columns, 60 wide, 3000 rows
-// 27.0 / 22.9, 4096 32.6 / 26.7 / 32.8, 16384 76.3 / 71.5 / 79.4; 3584, 64 wide, 2000 29.6 / 25.3 / 29.3, 8192 65.6 / 64.6 / 68.3; 4096, 8 wide,
-// 8192 55.3 / 51.2 / 56.5; 512, 8 wide, 16384 34.0 / 26.0; 1024, 256 wide, 2000 34.4 / 31.1; none of 35 sizes more than 1 % slower than
-// with 256).  The adapters have two sides and groups of different lengths, which few pieces divide unevenly, and want 512 (512 / 256, us:
-// 4096 x 4096, 8192 rows of 4, rank 16 76.5 / 81.9, of 8, rank 64 118 / 114, 4096 of 4, rank 64 74.5 / 67.2).  Few rows are not cut,
+// Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.  The router wants 256, beside which expand's
+// fill the units, and has half as many parts to join as with 512 (512 / 256, us: 8192 tokens of 3584, 64 experts 53.8 / 51.8); the
+// adapters, two sides and groups of different lengths, want 512 (8192 rows of 8, rank 64, 4096 x 4096 112 / 119).  Few rows are not cut,
 // which saves the launch that adds the pieces: up to 512 of one group for a P of up to 32 columns, 1024 of a wider one (2048 columns, cut /
-// not, us: 30 wide, 600 rows 11.7 / 11.3, 800 12.5 / 12.8; 60 wide, 600 15.5 / 11.9, 1024 17.3 / 14.9, 2000 20.3 / 22.7); twice as many of
-// several groups, among which they are seldom all one's (4 groups, 64 wide, 2000 rows 36.0 / 31.7, 4096 columns 49.9 / 39.5; all of one
-// group 35.5 / 46.7, 4096 columns 48.1 / 50.4).
+// not, us: 30 wide, 600 rows 12.0 / 11.7, 800 12.2 / 13.2; 60 wide, 600 15.4 / 12.6, 1024 17.0 / 14.4); twice as many of several
+// groups, among which they are seldom all one's (4 groups, 64 wide, 2000 rows 36.2 / 33.8; all of one group, 4096 columns 50 / 54).
 inline int outer_chunk(int T, int L, int tiles, int r, int want) {
   const int uncut = (r <= 32 ? 512 : 1024) * (L > 1 ? 2 : 1);
   if (T <= uncut) return uncut;
