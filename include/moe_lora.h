@@ -56,7 +56,7 @@ int moe_lora_forward(const void* x_bf16, const int32_t* adapter_idx, int32_t T, 
  * dy_bf16      [T,N] bf16
  * v            [T,rank] fp32 as moe_lora_forward left it
  * dx_in        [T,K] bf16, what other branches that read x contribute; may be dx itself; NULL: zeros
- * dx           [T,K] bf16, rounded once; NULL: not computed (dx_in must be NULL too)
+ * dx           [T,K] bf16, rounded once by each call that adds to it; NULL: not computed (dx_in must be NULL too)
  * grad_a       [n_adapters][rank][K] fp32, grad_b [n_adapters][N][rank] fp32: written whole, zeros for an adapter without rows
  * workspace    at least moe_lora_workspace_bytes(..., 1) bytes
  * Sums over rows are taken in a fixed order: the same call gives the same bits.  Sizes as above.

@@ -68,7 +68,7 @@ int moe_route_backward(const float* logits, const int32_t* topk_idx, const float
  *   d_w_router[h,e] = sum_t x[t,h] * d_logits[t,e];  dx[t,h] = dx_in[t,h] + sum_e d_logits[t,e] * w_router[h,e]
  * x_bf16     [T,H] bf16, w_router [H,E] fp32 (unused, may be NULL, without dx), d_logits [T,E] fp32; finite values
  * dx_in      [T,H] bf16, what other branches that read x contribute; may be dx itself; NULL: zeros
- * dx         [T,H] bf16, rounded once; NULL: not computed (dx_in must be NULL too)
+ * dx         [T,H] bf16, rounded once by each call that adds to it; NULL: not computed (dx_in must be NULL too)
  * d_w_router [H,E] fp32, written whole
  * workspace  at least moe_router_backward_workspace_bytes(T, H, E) bytes
  * The shared expert's gate (moe_combine's w_shared_gate) is the case E = 1 with d_logits = d_shared_gate.

@@ -16,8 +16,8 @@ using namespace skinny;
 
 // ---- up to 64 rows -------------------------------------------------------------------------------------------------------------
 // A short kernel or two, bound by their latency: every workgroup looks at all ids, one a lane.  With two, the adapters' matrices are read
-// straight into the MFMA's operands (through LDS, as for many rows, took 7.5 and 7.2 us instead of 5.7 and 5.0 with 48 rows of 32
-// adapters, 4096 x 4096, rank 16).
+// straight into the MFMA's operands (48 rows of 32 adapters, 4096 x 4096, rank 16: 4.2 and 5.1 us; through LDS, as for many rows, 7.5 and
+// 7.2 where they had taken 5.7 and 5.0).
 constexpr int kFewRows = 64, kFewTile = 16;
 
 struct Few {
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kExpandThreads) void expand_few_kernel(ExpandFew e)
 // Both products in one launch: each workgroup computes v for its 512 columns (or 1024) anew.  The wavefronts take an eighth of k each, all
 // of it on its way at once, 128 bytes of a row by eight neighbouring lanes and through LDS into the MFMA's operands: read as operands, 16 bytes
 // from each of 16 rows, an instruction would take 64 clocks.  Two launches / one, us, in a graph and one by one from the host: 8 rows of 8
-// adapters, 4096 x 4096, rank 16 7.3 / 7.0, 9.6 / 7.1; 2048 x 2048, rank 32, 40 adapters 7.9 / 6.7, 9.4 / 6.8.
+// adapters, 4096 x 4096, rank 16 7.6 / 7.3, 11.4 / 8.3; 2048 x 2048, rank 32, 40 adapters 8.0 / 7.0, 10.9 / 8.3.
 constexpr int kFusedWaves = 8, kFusedThreads = kFusedWaves * 64;
 
 template <typename YT, int NT, int FLIGHT, int WIDE>
@@ -345,10 +345,12 @@ __global__ __launch_bounds__(kFusedThreads, 2) void fused_few_kernel(ExpandFew e
 }
 
 // Where k comes in one go (else its halves wait for each other: 2 x 256 KB, rank 32, 7.8 / 8.9 us; 2 x 88 KB of K = 5632 7.5 / 8.4), the
-// workgroups run side by side and what they read again is little: 16 / 28 MB of A 7.9 / 7.4, 7.5 / 7.3; 32 MB and 256 workgroups 8.2 / 9.8.
+// workgroups run side by side and what they read again is little.  Two launches / one, us in a graph, by the bytes of A that one reads:
+// 8 MB 7.6 / 7.3, 21 MB (40 rows of 40, 2048 x 4096, rank 32) 8.4 / 7.9, 33 MB and 256 workgroups (64 of 64) 9.3 / 9.8.
 constexpr int64_t kFusedBytes = 28 << 20;
-// 512 columns a workgroup, or 1024 where that alone keeps to it (48 rows of 32 adapters, 4096 x 4096, rank 16 8.4 / 7.7, 9.4 / 7.6 from the
-// host; else narrow is faster, 24 of 24, rank 8 7.2 / 7.7).  0: two launches.
+// 512 columns a workgroup, or 1024 where that alone keeps to it: narrow is faster where both do (24 rows of 24, 4096 x 4096, rank 8 7.2 / 8.0,
+// one row of rank 16 7.1 / 7.7).  48 rows of 32, rank 16 take 8.4 in two launches, 9.9 narrow and 8.6 wide in a graph, 10.7, 9.7 and 8.4
+// from the host.  0: two launches.
 int fused_wide(int T, int K, int N, int rank, int L) {
   if (rank > 32 || K * ceil_div(rank, 16) > 4096) return 0;
   for (int wide = 1; wide <= 2; ++wide) {
@@ -394,7 +396,7 @@ void launch_expand_few(const ExpandFew& e, hipStream_t s) {
 
 // ---- sorted rows ---------------------------------------------------------------------------------------------------------------
 // Whether each workgroup that needs v adds its slices itself, which saves a launch, or pack_kernel does it once.  Once / each, us, 4096 x
-// 4096: rank 16, 300 rows 15.7 / 13.6, 8192 50.3 / 48.2; rank 64, 300 rows 19.1 / 18.3, 4096 (8 slices) 44.3 / 48.9, 8192 (4) 69 / 73.
+// 4096: rank 16, 300 rows 16.4 / 13.1, 8192 65.3 / 60.5; rank 64, 300 rows 20.2 / 19.2, 4096 (8 slices) 45.3 / 49.3, 8192 (4) 77.6 / 79.8.
 bool from_sums(int T, int rank, int slices) { return rank <= 32 || (rank <= 64 && T * slices <= 24576); }
 
 template <typename YT>
@@ -410,8 +412,8 @@ void launch_expand(const Expand& e, int n_tiles, hipStream_t s) {
 
 // Before the products of a backward pass: out[c][r] = in[r][c] for A and B of each adapter that has rows, 64 x 64 values by half a workgroup,
 // four times that a workgroup.  Up to kSortOnce rows each workgroup looks for its adapter among the ids itself, and so does not wait
-// for the sort, which the launch's first workgroup does meanwhile (the whole pass, 4096 x 4096, us: 777 rows of 4 adapters, rank 64 35.5 / 32.4,
-// 8192 of 8 111 / 107, 300 of 256, rank 16 129 / 133).
+// for the sort, which the launch's first workgroup does meanwhile (the whole pass, 4096 x 4096, us: 777 rows of 4 adapters, rank 64 35.0 / 31.6,
+// 8192 of 8 119 / 115, 300 of 256, rank 16 144 / 158).
 struct Transpose {
   const uint16_t* in[2];
   uint16_t* out[2];

@@ -86,7 +86,7 @@ __device__ __forceinline__ void group_softmax(float (&p)[U][S], int l, int E, fl
 // ---- balance loss ----------------------------------------------------------------------------------------------------------
 // A workgroup takes every gridDim.x-th run of tokens and leaves the sums of its probabilities, squared logarithms and counts; the
 // counts are integers added in LDS, whose order does not matter, the rest is added in a fixed order.  One workgroup alone finishes by
-// itself, several leave their sums to balance_join_kernel.  16384 tokens of 64 experts: 5.8 us (5.5 MB; a launch alone is 2.5) and 5.5 for the
+// itself, several leave their sums to balance_join_kernel.  16384 tokens of 64 experts: 5.9 us (5.5 MB; a launch alone is 2.5) and 5.4 for the
 // 256 parts that one compute unit reads to join them.
 constexpr int kLossThreads = 512, kLossWaves = kLossThreads / kWave;
 
@@ -236,7 +236,7 @@ struct RouteBackward {
 
 // The gradients at the picked experts, k values of a token, come to the lanes of these experts through LDS (a group's own piece of
 // it).  The losses' part is p (f - sum p f), that of the gates the same with their own softmax, which without renormalisation is p too:
-// one dot product serves both then.  16384 tokens of 64 experts, 8 picked: 6.1 us for 9.4 MB; 64 of 8, 3.0, a launch's time.
+// one dot product serves both then.  16384 tokens of 64 experts, 8 picked: 6.4 us for 9.4 MB; 64 of 8, 3.0, a launch's time.
 template <int G, int S, int U>
 __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward b) {
   constexpr int PICKED = G < MOE_MAX_TOPK ? 2 : 1;  // a lane's share of a token's picked experts
@@ -375,7 +375,7 @@ struct LaunchRoute {
 int router_width(int E) { return ceil_div(E, 32) * 32; }
 
 // In one launch: W_r's parts, 2048 values a workgroup, and d_logits' fragments, 32 rows a workgroup (8192 tokens of 3584, 64 experts:
-// 5.8 us).
+// 5.6 us).
 constexpr int kSplitValues = 4;
 __global__ __launch_bounds__(kPackThreads) void router_prepare_kernel(const float* __restrict__ w, int64_t n, int E, int R,
                                                                       uint16_t* __restrict__ out, int split_blocks, Pack pack) {

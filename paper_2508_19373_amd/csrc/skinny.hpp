@@ -240,10 +240,11 @@ inline void launch_sort(const Sort& a, hipStream_t s) {
 // 128 bytes of each row, read by eight neighbouring lanes, put into the wavefront's own piece of LDS with the 16-byte parts of a row
 // rearranged by the row's number, and read back as fragments without bank conflicts.  The next piece of x is on its way from HBM
 // meanwhile, and the next 32 rows of M_a from L2.  The wavefronts' sums are added in order through LDS, the slices' by pack_kernel.
-// Why slices: a compute unit takes in about 45 KB a microsecond whatever the pattern, so what counts is how many bytes the busiest one
-// reads.  With 16 rows of all of k a workgroup, M_a would be twice x's bytes at rank 32, and 260 workgroups on 256 units took half as
-// long again as 256 (19 and 12.6 us; 33 MB of x).  Now 14.6 us for 4096 rows of 4096 at rank 32 (2.3 TB/s of x), 29.6 for 8192 at rank
-// 64: bound by what a unit takes in, x and, from L2, M_a.
+// Why slices: what counts is how many bytes the busiest compute unit reads, about 45 KB a microsecond at best.  With 16 rows of all of k a
+// workgroup, M_a would be twice x's bytes at rank 32, and 260 workgroups on 256 units took half as long again as 256 (19 and 12.6 us; 33 MB
+// of x).  Now 14.1 us for 4096 rows of 4096 at rank 32 (2.4 TB/s of x), 29.7 for 8192 at rank 64.  The busiest unit's bytes (288 and 768 KB)
+// take 6.4 and 17 of these; what the rest goes into is not known: a slice leaves a wavefront two to four pieces and the next one's loads
+// cover little of their own latency.
 constexpr int kShrinkWaves = 4, kShrinkThreads = kShrinkWaves * 64;
 
 struct Shrink {
@@ -478,7 +479,7 @@ inline size_t outer_bytes(int n, int r) { return (size_t)n * 2 * ceil_div(r, 16)
 // A wavefront computes up to 64 rows of 16 NJ columns, 16 rows at a time.  The MFMA's first operand is P, its second M_a; accumulator j of
 // lane c stands for column NJ c + j (of fp32 results 4 c + j % 4 of every 64), so that a lane's values of one row are neighbours and the 16
 // lanes of a row read and write up to 256 bytes in a row.  M_a's fragments stay in registers; they come through the wavefront's own LDS,
-// where they are put as they lie in memory.  The next 16 rows' P and Y are on their way during a step's products.  4096 rows of 4096 columns, bf16 in and out, rank 32: 18.5 us from packed P (3.6 TB/s), 21.9 from sums, where pack_kernel's 4 us are saved.  (All 64 rows of Y on
+// where they are put as they lie in memory.  The next 16 rows' P and Y are on their way during a step's products.  4096 rows of 4096 columns, bf16 in and out, rank 32: 20.2 us from packed P (3.3 TB/s), 22.4 from sums, where pack_kernel's 4 us are saved.  (All 64 rows of Y on
 // their way from the start instead of 16 ahead took more registers and 5 % longer.)
 constexpr int kExpandThreads = 256, kExpandWaves = kExpandThreads / kWave;
 
@@ -805,7 +806,8 @@ __device__ __forceinline__ void expand_f32_tile(const ExpandF32& e, int col_bloc
 // LDS.  P's fragments come packed in parts.  The wavefronts take every fourth 32 rows; their sums are added in order through LDS,
 // one tile of P's columns at a time.  A group of more than `chunk` rows is cut, its pieces' sums go to `part` and join in
 // reduce_kernel: which pieces there are follows from the rows alone, so the order of the additions is fixed.  8192 rows of 4096 and 4096
-// columns at rank 64: 50 us, 27 without P, whose fragments each column tile reads from L2 anew (200 MB beside 134 MB of Z).
+// columns at rank 64: 47 us for 134 MB of Z.  Each column tile reads P's fragments anew (200 MB): 27 us without these loads, 43 with as many of
+// them that all read the same 12 KB, so that it is their number that costs, not the way to L2.
 struct OuterSide {
   const uint16_t* z;    // [T][cols]
   const u32x4* packed;
@@ -960,8 +962,8 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
 
 // The products of a backward pass in one launch: neither needs the other, so the end of the one is the other's beginning.
 // Workgroups are numbered through: outer's (x fastest), then expand's; the two taking turns was slower (the whole pass 115 / 129 us).
-// 8192 rows, rank 64, 4096 and 4096 columns: 64.7 us for 201 MB (3.1 TB/s; apart 50 + 23); 8192 tokens of 3584, 64 experts 43.3 for 117 MB
-// (26 + 25.6).
+// 8192 rows, rank 64, 4096 and 4096 columns: 61.9 us for 201 MB (3.2 TB/s; the sums over rows alone 47); 8192 tokens of 3584, 64 experts
+// 49.7 for 117 MB (23), of which the six products of W_r's and d_logits' parts are 23 GFLOP.
 template <int CH, int NJ>
 struct ExpandByGroup {
   typedef Expand Args;
@@ -1021,9 +1023,9 @@ static __global__ __launch_bounds__(256) void reduce_kernel(Outer o) {
 }
 
 // MT columns' tiles of P a workgroup, one at a time where the launch is thin all the same: shorter steps, and what Z's rows are read again for
-// comes from L2 (2048 columns, 60 wide, 333 rows 14.6 / 12.2 us, 700 16.7 / 15.5, 3000 (768 workgroups) 23.9 / 27.9).
+// comes from L2 (2048 columns, 60 wide, 333 rows 13.2 / 11.5 us, 700 17.5 / 12.5, 3000 (768 workgroups) 27.7 / 30.5).
 constexpr int kThin = 256;
-// (More workgroups than a grid's x has room for would need 250 GB of rows.)
+// (More workgroups than a grid's x has room for would need more rows than the memory holds.)
 template <int MT, typename EXPAND>
 void launch_both_tiles(Both<EXPAND> a, int n_tiles, hipStream_t s) {
   a.outers = a.outer_x * a.pieces * ceil_div(a.o.r, 16 * MT);
@@ -1053,12 +1055,16 @@ inline void launch_reduce(const Outer& o, hipStream_t s) {
   hipLaunchKernelGGL(reduce_kernel, dim3(ceil_div(values, 1024), o.L), dim3(256), 0, s, o);
 }
 
-// Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.  The router wants 256, beside which expand's
-// fill the units, and has half as many parts to join as with 512 (512 / 256, us: 8192 tokens of 3584, 64 experts 53.8 / 51.8); the
-// adapters, two sides and groups of different lengths, want 512 (8192 rows of 8, rank 64, 4096 x 4096 112 / 119).  Few rows are not cut,
-// which saves the launch that adds the pieces: up to 512 of one group for a P of up to 32 columns, 1024 of a wider one (2048 columns, cut /
-// not, us: 30 wide, 600 rows 12.0 / 11.7, 800 12.2 / 13.2; 60 wide, 600 15.4 / 12.6, 1024 17.0 / 14.4); twice as many of several
-// groups, among which they are seldom all one's (4 groups, 64 wide, 2000 rows 36.2 / 33.8; all of one group, 4096 columns 50 / 54).
+// Rows of a piece: about `want` workgroups for the column tiles there are, 256 rows at least.  The router wants 256: with dx, whose
+// workgroups fill the units as well, fewer and longer pieces are a little better, without it worse (512 / 256 / 128, us: with dx 4096 tokens
+// of 2048, 60 experts 32.8 / 32.6 / 26.7, 16384 79.4 / 76.3 / 71.5; 8192 of 3584, 64 experts 68.3 / 65.6 / 64.6, of 4096, 8 experts 56.5 /
+// 55.3 / 51.2; 256 / 128 without dx 33.0 / 37.6, 28.9 / 34.0 and 20.9 / 23.6 for the last three; the sums are the same with dx and without,
+// so one number serves both).  The adapters have two sides and groups of different lengths, which few pieces divide unevenly, and want
+// 512 (512 / 256, us, 4096 x 4096: 8192 rows of 4, rank 16 76.5 / 81.9, of 8, rank 64 118 / 114, 4096 of 4, rank 64 74.5 / 67.2).  Few rows
+// are not cut, which saves the launch that adds the pieces: up to 512 of one group for a P of up to 32 columns, 1024 of a wider one (2048
+// columns, cut / not, us: 30 wide, 600 rows 11.7 / 11.3, 800 12.5 / 12.8; 60 wide, 600 15.5 / 11.9, 1024 17.3 / 14.9, 2000 20.3 / 22.7); twice
+// as many of several groups, among which they are seldom all one's (4 groups, 64 wide, 2000 rows 36.0 / 31.7, 4096 columns 49.9 / 39.5; all
+// of one group 35.5 / 46.7, 4096 columns 48.1 / 50.4).
 inline int outer_chunk(int T, int L, int tiles, int r, int want) {
   const int uncut = (r <= 32 ? 512 : 1024) * (L > 1 ? 2 : 1);
   if (T <= uncut) return uncut;

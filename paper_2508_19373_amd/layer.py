@@ -465,6 +465,7 @@ class ExpertShardLayer:
     def _add_adapters(self, x, adapter_idx, T, stream):
         if adapter_idx is None or self.adapters is None:
             return
+        # (a bf16 y_out is rounded by the combine and once more here: 1.77e-3 from the fp32 output instead of 1.66e-3, 333 tokens of 512)
         L, rank, _ = self.adapters.a.shape
         B.moe_lora_forward(x, adapter_idx, T, self.H, self.H, rank, L, *self.adapters, self.y_out, self.y_out, self.lora_v,
                            self.lora_ws, B.MOE_OUT_F32 if self.out_f32 else 0, stream)
@@ -525,6 +526,9 @@ class ExpertShardLayer:
             self.router_losses(token_mask, stream)
         B.moe_route_backward(self.logits, self.topk_idx, self.d_topk_w, token_mask, self.counts if losses else None, T, E, self.k,
                              coef_balance, coef_z, B.MOE_RENORM_TOPK if self.renorm else 0, self.d_logits, stream)
+        # Each branch adds its part to dx and rounds the sum to bf16, half a step every time, as a caller's own chain of such calls does.  The
+        # adapters' part, as a rule the largest, comes last (333 tokens of 512, rel-L2 from 64 bits: router 1.66e-3, with the gate 2.21e-3,
+        # with adapters 1.70e-3, all three 1.73e-3; one rounding alone 1.66e-3).
         dx = self.dx if need_dx else None
         router = self.w_router is not None and self._own_logits
         if router:
