@@ -397,6 +397,12 @@ __global__ __launch_bounds__(kPackThreads) void router_prepare_kernel(const floa
   }
 }
 
+// Above 64 experts dx's workgroups take W_r's columns in several rounds.  While they are few, one after the other bound by a round's latency,
+// they have half the columns and four rounds' loads on their way; else P, which each of them reads, counts (workgroups: us with half the
+// columns / with all: 1024 columns, 256 experts 4: 18.8 / 25.1, 32: 21.7 / 28.1, 188: 40.6 / 37.4, 1024: 120 / 107; 2048, 128 experts
+// 8: 12.3 / 15.6, 64: 14.4 / 17.3, 376: 34.3 / 35.9, 1024: 61.4 / 57.6).
+constexpr int kFewF32 = 128;
+
 struct RouterPlan {
   int chunk, pieces, slots, tiles;
   size_t split, packed, outer, partial, bytes;  // offsets in the workspace
@@ -587,9 +593,11 @@ int moe_router_backward(const void* x_bf16, const float* w_router, const float* 
                 E, p.chunk};
   if (dx != nullptr && T > 0) {
     const ExpandF32 e{T, packed, E, split, H, static_cast<const uint16_t*>(dx_in), static_cast<uint16_t*>(dx)};
-    if (E <= 16) launch_both<1, ExpandByF32>(o, p.pieces, e, p.tiles, s);
-    else if (E <= 32) launch_both<2, ExpandByF32>(o, p.pieces, e, p.tiles, s);
-    else launch_both<4, ExpandByF32>(o, p.pieces, e, p.tiles, s);
+    if (E <= 16) launch_both<1, ExpandByF32<4, 1, false>>(o, p.pieces, e, p.tiles, s);
+    else if (E <= 32) launch_both<2, ExpandByF32<4, 1, false>>(o, p.pieces, e, p.tiles, s);
+    else if (E <= 64) launch_both<4, ExpandByF32<4, 2, false>>(o, p.pieces, e, p.tiles, s);
+    else if (p.tiles * ceil_div(H, ExpandByF32<4, 1, true>::kCols) <= kFewF32) launch_both<4, ExpandByF32<2, 4, true>>(o, p.pieces, e, p.tiles, s);
+    else launch_both<4, ExpandByF32<4, 1, true>>(o, p.pieces, e, p.tiles, s);
   } else {
     launch_outer(o, p.pieces, s);
   }

@@ -706,8 +706,10 @@ void launch_expand_kernel(const Expand& e, int n_tiles, hipStream_t s) {
 // ---- expand by an fp32 matrix --------------------------------------------------------------------------------------------------
 // The same where M is fp32 too (the router's weights) and all rows are one group.  P and M are three bf16 parts each, all 24 bits of
 // either; of the nine products of parts the three below 2^-23 of the whole are left out, so that the sums are as exact as fp32 products'.
-// A wavefront has 64 columns of all 64 rows in its accumulators and takes 32 of M's columns after the other, the next ones on their way
-// meanwhile.  P's parts lie in LDS, where the workgroup's four wavefronts share them.
+// A wavefront has 16 NJ columns of all 64 rows in its accumulators and takes 32 of M's columns after the other, AHEAD of them on their way at
+// once (LOOP: there are more than AHEAD).  P's parts lie in LDS, where the workgroup's four wavefronts share them.  Up to 64 columns come in one
+// go, which leaves registers for a third workgroup on a compute unit where it is 32 (2048 columns, one wide, 3000 rows 19.1 us instead of
+// 21.1 with the loop's code, one row 7.3 instead of 7.8).
 struct ExpandF32 {
   int T;
   const u32x4* packed;   // [tiles][4][chunks of 32 columns][kParts][64]
@@ -717,32 +719,34 @@ struct ExpandF32 {
   const uint16_t* y_in;  // [T][N] or nullptr
   uint16_t* y_out;       // [T][N]
 };
-constexpr int kF32Cols = 64, kF32Fragments = kTileRows / 16 * kParts;  // columns of a wavefront; P's fragments of 32 columns
-constexpr int kExpandF32Bytes = (2 * kF32Fragments + kExpandWaves * kF32Cols / 16) * 1024;
+constexpr int kF32Fragments = kTileRows / 16 * kParts;  // of P, for 32 columns
 
+template <int NJ, int AHEAD, bool LOOP>
 __device__ __forceinline__ void expand_f32_tile(const ExpandF32& e, int col_block, int which, char* s_buf) {
-  constexpr int NJ = kF32Cols / 16, U = kTileRows / 16, ITEMS = kF32Fragments / kExpandWaves;
+  constexpr int U = kTileRows / 16, ITEMS = kF32Fragments / kExpandWaves;
   static_assert(kF32Fragments % kExpandWaves == 0, "the wavefronts bring as many fragments each");
+  typedef uint32_t unit __attribute__((ext_vector_type(NJ / 2)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ln = lane & 15, q = lane >> 4;
   const int first = which * kTileRows, rows = min(kTileRows, e.T - first), chunks = (e.r + 31) / 32;
-  const int nbase = (col_block * kExpandWaves + wave) * kF32Cols, c0 = nbase + NJ * ln;
+  const int nbase = (col_block * kExpandWaves + wave) * 16 * NJ, c0 = nbase + NJ * ln;
   u32x4* const s_p = reinterpret_cast<u32x4*>(s_buf);  // two of them in turns
-  char* const s_m = s_buf + 2 * kF32Fragments * 1024 + wave * kF32Cols * 64;
-  u32x4 m[kParts][NJ], p[ITEMS];
-  const auto load = [&](int c) {
+  char* const s_m = s_buf + 2 * kF32Fragments * 1024 + wave * NJ * 1024;
+  u32x4 m[AHEAD][kParts][NJ], p[AHEAD][ITEMS];
+  const auto load = [&](int at, int c) {
 #pragma unroll
     for (int pt = 0; pt < kParts; ++pt)
 #pragma unroll
       for (int i = 0; i < NJ; ++i)  // (past the last column: that one again, not stored)
-        m[pt][i] = *reinterpret_cast<const u32x4*>(
+        m[at][pt][i] = *reinterpret_cast<const u32x4*>(
             e.m + ((size_t)min(nbase + 16 * i + (lane >> 2), e.N - 1) * kParts + pt) * 32 * chunks + 32 * c + 8 * (lane & 3));
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const int f = i * kExpandWaves + wave;
-      p[i] = e.packed[((((size_t)which * U + f / kParts) * chunks + c) * kParts + f % kParts) * 64 + lane];
+      p[at][i] = e.packed[((((size_t)which * U + f / kParts) * chunks + c) * kParts + f % kParts) * 64 + lane];
     }
   };
-  load(0);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) load(i, min(i, chunks - 1));
   f32x4 acc[U][NJ];  // from y_in on; without it the same bytes of M again, not used (no load under a condition)
   const bool some = e.y_in != nullptr;
   const uint16_t* const in = some ? e.y_in + (size_t)first * e.N + min(c0, e.N - NJ) : e.m;
@@ -750,44 +754,48 @@ __device__ __forceinline__ void expand_f32_tile(const ExpandF32& e, int col_bloc
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const uint2 d = *reinterpret_cast<const uint2*>(in + (some ? (size_t)min(16 * u + 4 * q + k, rows - 1) * e.N : 0));
-      acc[u][0][k] = some ? bf16_lo(d.x) : 0.f;
-      acc[u][1][k] = some ? bf16_hi(d.x) : 0.f;
-      acc[u][2][k] = some ? bf16_lo(d.y) : 0.f;
-      acc[u][3][k] = some ? bf16_hi(d.y) : 0.f;
+      const unit d = *reinterpret_cast<const unit*>(in + (some ? (size_t)min(16 * u + 4 * q + k, rows - 1) * e.N : 0));
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[u][j][k] = some ? (j & 1 ? bf16_hi(d[j / 2]) : bf16_lo(d[j / 2])) : 0.f;
     }
-  for (int c = 0; c < chunks; ++c) {
-    u32x4* const parts = s_p + (c & 1) * kF32Fragments * 64;
+  for (int first_c = 0; first_c < chunks; first_c += AHEAD) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) parts[(i * kExpandWaves + wave) * 64 + lane] = p[i];
-    u32x4 w[kParts][NJ];
+    for (int at = 0; at < AHEAD; ++at) {
+      const int c = first_c + at;
+      if (AHEAD > 1 && c >= chunks) break;
+      u32x4* const parts = s_p + (c & 1) * kF32Fragments * 64;
 #pragma unroll
-    for (int pt = 0; pt < kParts; ++pt) {
+      for (int i = 0; i < ITEMS; ++i) parts[(i * kExpandWaves + wave) * 64 + lane] = p[at][i];
+      u32x4 w[kParts][NJ];
 #pragma unroll
-      for (int i = 0; i < NJ; ++i) {  // column n: accumulator n % NJ of lane n / NJ
-        const int n = 16 * i + (lane >> 2), l = n / NJ;
-        *reinterpret_cast<u32x4*>(s_m + (n % NJ * 16 + l) * 64 + (((lane & 3) ^ (l >> 1 & 3)) * 16)) = m[pt][i];
+      for (int pt = 0; pt < kParts; ++pt) {
+#pragma unroll
+        for (int i = 0; i < NJ; ++i) {  // column n: accumulator n % NJ of lane n / NJ
+          const int n = 16 * i + (lane >> 2), l = n / NJ;
+          *reinterpret_cast<u32x4*>(s_m + (n % NJ * 16 + l) * 64 + (((lane & 3) ^ (l >> 1 & 3)) * 16)) = m[at][pt][i];
+        }
+        wave_fence();
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) w[pt][j] = *reinterpret_cast<const u32x4*>(s_m + (j * 16 + ln) * 64 + ((q ^ (ln >> 1 & 3)) * 16));
+        wave_fence();
       }
-      wave_fence();
+      __syncthreads();  // (one is enough: `parts` is written again only after the next one)
+      if (LOOP && c + AHEAD < chunks) load(at, c + AHEAD);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) w[pt][j] = *reinterpret_cast<const u32x4*>(s_m + (j * 16 + ln) * 64 + ((q ^ (ln >> 1 & 3)) * 16));
-      wave_fence();
+      for (int u = 0; u < U; ++u) {
+        if (16 * u >= rows) break;
+        u32x4 a[kParts];
+#pragma unroll
+        for (int s = 0; s < kParts; ++s) a[s] = parts[(u * kParts + s) * 64 + lane];
+#pragma unroll
+        for (int sum = kParts - 1; sum >= 0; --sum)  // the small products first
+#pragma unroll
+          for (int s = sum; s >= 0; --s)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[u][j] = mfma(a[s], w[sum - s][j], acc[u][j]);
+      }
     }
-    __syncthreads();  // (one is enough: `parts` is written again only after the next one)
-    if (c + 1 < chunks) load(c + 1);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (16 * u >= rows) break;
-      u32x4 a[kParts];
-#pragma unroll
-      for (int s = 0; s < kParts; ++s) a[s] = parts[(u * kParts + s) * 64 + lane];
-#pragma unroll
-      for (int sum = kParts - 1; sum >= 0; --sum)  // the small products first
-#pragma unroll
-        for (int s = sum; s >= 0; --s)
-#pragma unroll
-          for (int j = 0; j < NJ; ++j) acc[u][j] = mfma(a[s], w[sum - s][j], acc[u][j]);
-    }
+    if (!LOOP) break;
   }
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -795,8 +803,10 @@ __device__ __forceinline__ void expand_f32_tile(const ExpandF32& e, int col_bloc
     for (int k = 0; k < 4; ++k) {
       const int row = 16 * u + 4 * q + k;
       if (row >= rows || c0 >= e.N) continue;
-      *reinterpret_cast<uint2*>(e.y_out + (size_t)(first + row) * e.N + c0) =
-          make_uint2(pack_bf16x2(acc[u][0][k], acc[u][1][k]), pack_bf16x2(acc[u][2][k], acc[u][3][k]));
+      unit o;
+#pragma unroll
+      for (int i = 0; i < NJ / 2; ++i) o[i] = pack_bf16x2(acc[u][2 * i][k], acc[u][2 * i + 1][k]);
+      *reinterpret_cast<unit*>(e.y_out + (size_t)(first + row) * e.N + c0) = o;
     }
 }
 
@@ -972,11 +982,12 @@ struct ExpandByGroup {
     expand_tile<uint16_t, CH, NJ>(e, col_block, which, s_rows, s_buf);
   }
 };
+template <int NJ, int AHEAD, bool LOOP>
 struct ExpandByF32 {
   typedef ExpandF32 Args;
-  static constexpr int kCols = kExpandWaves * kF32Cols, kBytes = kExpandF32Bytes;
+  static constexpr int kCols = kExpandCols * NJ, kBytes = (2 * kF32Fragments + kExpandWaves * NJ) * 1024;
   static __device__ __forceinline__ void run(const Args& e, int col_block, int which, int32_t*, char* s_buf) {
-    expand_f32_tile(e, col_block, which, s_buf);
+    expand_f32_tile<NJ, AHEAD, LOOP>(e, col_block, which, s_buf);
   }
 };
 template <typename EXPAND>

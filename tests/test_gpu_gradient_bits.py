@@ -78,7 +78,7 @@ def test_adapters_dx(T, K, N, r, L):
 
 
 @pytest.mark.parametrize("T,H,E", [(1, 64, 1), (65, 520, 8), (300, 264, 20), (333, 2048, 60), (200, 1032, 64), (130, 520, 100), (65, 264, 200),
-                                   (70, 136, 256)])
+                                   (70, 136, 256), (2100, 1032, 100), (2500, 1032, 256)])
 def test_routers_dx(T, H, E):
     print("case bits of the router's dx", T, H, E, flush=True)
     g = torch.Generator().manual_seed(T + E)
