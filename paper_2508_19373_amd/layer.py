@@ -2,6 +2,7 @@
 and issues the C-ABI calls in order.  No arithmetic happens here."""
 from __future__ import annotations
 
+import contextlib
 from typing import NamedTuple
 
 import numpy as np
@@ -48,6 +49,13 @@ def _side_stream(device):
     if key not in _SIDE_STREAMS:
         _SIDE_STREAMS[key] = torch.cuda.Stream(device=device)
     return _SIDE_STREAMS[key]
+
+
+def _on(stream):
+    """Torch's own work on the caller's stream: None (the current one), a torch stream or a raw one."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
 
 
 def routed_hint_beside_shared(ffn_shard, shared_shard, T) -> int:
@@ -409,7 +417,8 @@ class ExpertShardLayer:
             self.lora_ws = torch.empty(self._lora_bytes(T), dtype=torch.uint8, device=self.device)
         flags = B.MOE_RENORM_TOPK if self.renorm else 0
         if logits is not None:
-            self.logits[:T].copy_(logits)
+            with _on(stream):
+                self.logits[:T].copy_(logits)
             flags |= B.MOE_LOGITS_GIVEN
         yflag = B.MOE_Y_PERM_BF16 if self.y_perm_bf16 else 0
         cflags = yflag | (B.MOE_OUT_F32 if self.out_f32 else 0)

@@ -38,3 +38,24 @@ def test_no_workspace_grows_inside_a_capture(monkeypatch):
     with pytest.raises(RuntimeError):
         layer.forward(x, adapter_idx=idx)
     assert layer.lora_ws is small
+
+
+def test_given_logits_are_copied_on_the_callers_stream(monkeypatch):
+    """Not on torch's current one, beside which the caller's would read them half written."""
+    layer, used = _layer(max_tokens=4), []
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            used.append(self.stream)
+
+        def __exit__(self, *_):
+            used.append(None)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    stream = object()
+    with pytest.raises(ValueError):
+        layer.forward(_x(4)[0], torch.ones(4, 2), stream=stream)
+    assert used == [stream, None] and bool((layer.logits[:4] == 1).all())

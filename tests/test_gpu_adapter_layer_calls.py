@@ -98,3 +98,28 @@ def test_sliced_down_projections_adapters_add_up(T, overlap):
     assert not torch.equal(without, want)
     total = sum(_layer(w, down=True, tp=2, p=p, out_f32=True, overlap_shared=overlap).forward(x, adapter_idx=idx).clone() for p in range(2))
     assert _rel(total, want) <= 1e-4        # as test_shards_add_up
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("T", [7, 160])
+def test_a_step_on_a_stream_of_the_callers(T, given):
+    """Forward, losses and backward with stream=: the same bits as on torch's current stream, which is busy meanwhile."""
+    w = _weights()
+    x, dy, idx, mask = _batch(T)
+    logits = torch.randn(T, E, device="cuda") if given else None
+    one, other = _layer(w, overlap_shared=False, max_tokens=T), _layer(w, overlap_shared=False, max_tokens=T)
+    other._alloc_grad(T)
+    other.logits.zero_()
+    want = (one.forward(x, logits, adapter_idx=idx), *one.backward(x, dy, idx, mask, 0.5, 0.25), one.losses)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    torch.cuda._sleep(20_000_000)
+    got = (other.forward(x, logits, stream=stream, adapter_idx=idx), *other.backward(x, dy, idx, mask, 0.5, 0.25, stream=stream), other.losses)
+    stream.synchronize()
+    copies = []
+    with torch.cuda.stream(stream):
+        for t in got:
+            copies.append(None if t is None else t.clone())
+    torch.cuda.synchronize()
+    for a, b in zip(copies, want):
+        assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
