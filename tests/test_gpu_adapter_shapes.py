@@ -127,3 +127,15 @@ def test_slots_without_an_adapter_may_hold_anything(T, K, N, r):
     for a, b in zip(got, want):
         assert torch.equal(a, b)
     assert not any(t[i].any() for t in got[3:] for i in (0, 4))
+
+
+@pytest.mark.parametrize("T,K,N,r,L,kind", [(3, 262144, 262144, 8, 2, "one"), (70, 262144, 1032, 16, 2, "mixed"), (70, 1032, 262144, 24, 2, "mixed"),
+                                            (2, 8, 8, 8, 256, "mixed"), (64, 8, 8, 128, 256, "mixed"), (300, 8, 8, 120, 256, "mixed"),
+                                            (8193, 64, 64, 16, 256, "mixed"), (9000, 64, 64, 16, 255, "runs")])
+def test_at_the_limits(T, K, N, r, L, kind):
+    """The most columns, the fewest, the most adapters, on either side of the rows that one sort keeps in registers."""
+    print("case limits", T, K, N, r, L, kind, flush=True)
+    host = _make(T, T, K, N, r, L, kind)
+    d = {n: t.cuda() if torch.is_tensor(t) else t for n, t in host.items()}
+    _forward(d, True)
+    _backward(d, _forward(d, False))

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_gpu_router_grad as whole
 from paper_2508_19373_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +66,13 @@ def test_data_parallel_devices_sum_their_counts(T, E, k):
     total = counted(parts[0]) + counted(parts[1])
     assert torch.equal(total, counted(whole)) and int(total[E]) == int(mask.sum())
     assert torch.equal(torch.cat([gradient(p, total) for p in parts]), gradient(whole, total))
+
+
+@pytest.mark.parametrize("T,H,E", [(2, 262144, 8), (70, 262144, 64), (65, 262144, 1), (33, 8, 256)])
+def test_routers_product_at_the_limits(T, H, E):
+    whole.test_router_backward(T, H, E)
+
+
+@pytest.mark.parametrize("T,H,k,bf16,shared", [(2, 262144, 16, False, True), (3, 262144, 1, True, True)])
+def test_combines_gates_at_the_limits(T, H, k, bf16, shared):
+    whole.test_combine_backward(T, H, k, bf16, shared)
