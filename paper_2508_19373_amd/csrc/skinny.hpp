@@ -972,8 +972,8 @@ __global__ __launch_bounds__(kOuterThreads, 2) void outer_kernel(Outer o) {
 
 // The products of a backward pass in one launch: neither needs the other, so the end of the one is the other's beginning.
 // Workgroups are numbered through: outer's (x fastest), then expand's; the two taking turns was slower (the whole pass 115 / 129 us).
-// 8192 rows, rank 64, 4096 and 4096 columns: 61.9 us for 201 MB (3.2 TB/s; the sums over rows alone 47); 8192 tokens of 3584, 64 experts
-// 49.7 for 117 MB (23), of which the six products of W_r's and d_logits' parts are 23 GFLOP.
+// 8192 rows, rank 64, 4096 and 4096 columns: 64.0 us for 201 MB (3.1 TB/s; the sums over rows alone 47); 8192 tokens of 3584, 64 experts
+// 51 for 117 MB (23), of which the six products of W_r's and d_logits' parts are 23 GFLOP.
 template <int CH, int NJ>
 struct ExpandByGroup {
   typedef Expand Args;

@@ -480,7 +480,7 @@ class ExpertShardLayer:
                            self.lora_ws, B.MOE_OUT_F32 if self.out_f32 else 0, stream)
 
     def _add_shared_adapters(self, adapter_idx, T, stream):
-        """Beside the shared expert's down projection, from the rows that it read."""
+        """Beside the shared expert's down projection, from the rows that it read (a bf16 y_shared is rounded by both)."""
         if adapter_idx is None or self.shared_adapters is None:
             return
         L, rank, K = self.shared_adapters.a.shape
@@ -502,11 +502,11 @@ class ExpertShardLayer:
                  token_mask: torch.Tensor | None = None, coef_balance: float = 0.0, coef_z: float = 0.0,
                  dx_in: torch.Tensor | None = None, need_dx: bool = True, stream=None) -> Gradients:
         """Gradients of the last forward, of the same x and adapter_idx, for dy [T,H] bf16 and the router's losses times their
-        coefficients.  The experts' own weights are frozen, and so are the shared_adapters.  dx holds what reaches x through the router (not after given logits,
-        whose gradient is Gradients.logits), the shared expert's gate and the module's adapters, added to dx_in, the part through the
-        experts, which the caller brings: nothing here computes it.  After a forward with adapter_idx a call without needs
-        need_dx=False: the router and the gate alone are trained then.  A shard's gradients are its part of a sum: those of all
-        shards, the losses' coefficients given to one of them, add up to the unsharded layer's."""
+        coefficients.  The experts' own weights are frozen, and so are the shared_adapters.  dx holds what reaches x through the router
+        (not after given logits, whose gradient is Gradients.logits), the shared expert's gate and the module's adapters, added to
+        dx_in, the part through the experts, which the caller brings: nothing here computes it.  After a forward with adapter_idx a
+        call without needs need_dx=False: the router and the gate alone are trained then.  A shard's gradients are its part of a sum:
+        those of all shards, the losses' coefficients given to one of them, add up to the unsharded layer's."""
         T, H, E = self._rows(), self.H, self.E
         if token_mask is not None:
             self._check_rows(token_mask, "token_mask", (T,), torch.uint8)
